@@ -36,6 +36,9 @@ What it computes (StarSD, "One-for-Many Speculative Decoding"):
 * :mod:`oracle.expand` -- the draft side's layer expansion (Algorithm 2,
   ExpandLayer): top-k children per frontier node with their draft
   probabilities.  By definition.
+* :mod:`oracle.fp8` -- the 8-bit calls: e4m3 codes, block scales, the cache's
+  append and rows (its attention is the chain or tree attention on those rows),
+  the normed rows and the scaled projection.  By definition; imported by name.
 * :mod:`oracle.model` -- the performance model of Sec. 3 and Sec. 4.2: the
   acceptance rate beta (sum of min(p, q)), the expected accept length from
   the distribution of the accept length, and the per-iteration time, idle

@@ -1,7 +1,8 @@
 """Batched, lossless speculative verification on one MI355X (gfx950).
 
 Thin ctypes binding of ``libsdverify.so`` (the C-ABI declared in
-``include/sdverify.h``).  Each function has the C name, marshals torch device
+``include/sdverify.h``, and for 8-bit caches and weights in
+``include/sdverify_fp8.h``).  Each function has the C name, marshals torch device
 tensors, host integer arrays and the current HIP stream into the C call, and
 raises :class:`SdError` on a non-zero status.  No step of the computation runs
 in Python: every result comes from the HIP kernels, and the binding fails
@@ -55,4 +56,16 @@ from ._binding import (  # noqa: F401
     sd_vocab_kernel_name,
     sd_vocab_packed_bytes,
     sd_workspace_bytes,
+)
+from ._fp8 import (  # noqa: F401
+    SD_FP8_BLOCK,
+    SD_KV8_BLOCK,
+    KV8Cache,
+    Norm,
+    exported_fp8_symbols,
+    sd_fp8_workspace_bytes,
+    sd_kv8_append,
+    sd_residual_norm_fp8,
+    sd_verify_attention_kv8,
+    sd_verify_logits_fp8,
 )

@@ -16,7 +16,9 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libsdverify.so")
-SOURCES = ["api.hip", "attention.hip", "vocab.hip", "lines.hip", "rows.hip", "accept.hip", "warp.hip", "rate.hip", "pool.hip", "expand.hip"]
+SOURCES = ["api.hip", "attention.hip", "vocab.hip", "lines.hip", "rows.hip", "accept.hip", "warp.hip", "rate.hip", "pool.hip", "expand.hip",
+           "kv8_append.hip", "kv8_attention.hip", "norm_fp8.hip", "vocab_fp8.hip"]
+HOST_SOURCES = ["fp8_api.hip"]  # no kernels of their own
 ARCH = "gfx950"
 
 HIPCC_FLAGS = [
@@ -37,6 +39,8 @@ HIPCC_FLAGS = [
 # (masking uses -inf, never NaN; NaN-sensitive decisions live in accept.hip).
 EXTRA_FLAGS = {
     "attention.hip": ["-fno-honor-nans", "-mno-amdgpu-ieee"],
+    # The same for 8-bit caches; their NaN codes are found with integer operations.
+    "kv8_attention.hip": ["-fno-honor-nans", "-mno-amdgpu-ieee"],
 }
 
 
@@ -71,8 +75,9 @@ def build(verbose: bool = False) -> str:
         _run([hipcc, *HIPCC_FLAGS, *EXTRA_FLAGS.get(src, []), "-c", os.path.join(CSRC, src), "-o", obj], verbose)
         return obj
 
-    with ThreadPoolExecutor(min(len(SOURCES), os.cpu_count() or 1)) as ex:
-        objs = list(ex.map(compile_one, SOURCES))
+    sources = SOURCES + HOST_SOURCES
+    with ThreadPoolExecutor(min(len(sources), os.cpu_count() or 1)) as ex:
+        objs = list(ex.map(compile_one, sources))
     tmp = LIB + ".tmp"
     _run([hipcc, f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", tmp, *objs], verbose)
     os.replace(tmp, LIB)

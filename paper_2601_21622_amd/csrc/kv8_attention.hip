@@ -1,0 +1,527 @@
+// Verification attention over a paged 8-bit cache (split-KV) for gfx950.
+//
+//   O = softmax(scale * Q K^T + mask) V,  K = code * 2^e of its 64-key block and head, V likewise.
+//
+// The G * group queries that share a KV head are the rows of one KV head.  One
+// wave per work item (chunk of whole 64-key blocks of one request, KV head,
+// group of rows), four independent items per workgroup; each item writes a
+// partial (maximum, sum, O) and the merge joins them in chunk order.
+//
+// The cache is laid out in the order in which the matrix instructions take
+// their operands (sdverify_fp8.h): a lane's 16 bytes of K are two 32-wide steps
+// of one key, its 16 bytes of V four keys in each of the block's four 16-key
+// score tiles.  So K and V go from HBM into registers in loads of 1 KB in a row
+// each, with no LDS and no transposition: the probabilities that a lane holds
+// after S^T = K Q^T (tile t: keys 16 t + 4 g + r of group g = lane / 16) are the
+// keys that its V bytes hold, which is all that O^T += V^T P^T needs.  Codes
+// widen to bfloat16 with the block's scale in the same instruction, exactly.
+// (The 8-bit matrix instructions would skip that, but they keep too few bits:
+// sums of 128 products come out 1.4e-5 off, and P would have to be 8 bits.)
+//
+// The next block's K is loaded when the current one's scores are done, its V
+// when the products with V are: each has half a block's work to arrive.
+// Softmax in the log2 domain.  O is never rescaled (a branch that does so made
+// the compiler spill up to 535 registers): the chunk's first block sets each
+// row's reference maximum, and later scores may exceed it by 2^64, far within
+// float32 and bfloat16.  A row that outgrows that makes the wave take the maxima
+// of all blocks from there on and start its item again, once.
+#include <atomic>
+
+#include "fp8.h"
+
+namespace sdv {
+
+namespace {
+
+constexpr int kItems = 4;        // waves, and items, per workgroup
+constexpr int kMaxBlocks = 5;    // 16-row blocks per wave
+constexpr int kMaxTiles = 64;    // blocks per chunk: one lane holds one block's page
+constexpr float kGrowLog2 = 64.f;  // growth of a row's maximum that takes the item up anew
+
+typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
+typedef __attribute__((__vector_size__(2 * sizeof(float)))) float f32x2;
+
+__device__ __forceinline__ float max_over_groups(float v) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float sum_over_groups(float v) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+// Positions that position `lane` (< G) sees of the step's own (bit a: position
+// a): in a chain itself and those before it, in a tree itself and its
+// ancestors, by pointer jumping over the parents.
+__device__ __forceinline__ uint64_t position_mask(const int32_t* __restrict__ parent, int G) {
+  const int lane = threadIdx.x & 63;
+  if (parent == nullptr) return lane >= 63 ? ~0ull : (2ull << lane) - 1ull;
+  int p = 0;
+  if (lane > 0 && lane < G) {
+    const int pp = parent[lane - 1];
+    p = (pp >= -1 && pp < lane - 1) ? pp + 1 : 0;
+  }
+  uint64_t m = 1ull | (1ull << lane);
+#pragma unroll
+  for (int i = 0; i < 6; ++i) {
+    const uint32_t lo = __shfl((uint32_t)m, p), hi = __shfl((uint32_t)(m >> 32), p);
+    m |= ((uint64_t)hi << 32) | lo;
+    p = __shfl(p, p);
+  }
+  return m;
+}
+
+// Bytes of a dword of four keys, the first of them `key`, that lie before `end`.
+__device__ __forceinline__ uint32_t bytes_before(int key, int end) {
+  const int n = end - key;
+  return n >= 4 ? 0xffffffffu : n <= 0 ? 0u : (1u << (8 * n)) - 1u;
+}
+
+// 1 in each byte of a dword that is a NaN code.
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t codes) {
+  return (((codes & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7;
+}
+
+// Bit i: whether key `off` + i (counted from the first of the step's positions)
+// is seen: all keys before them, then the positions of `sees`, none after.
+__device__ __forceinline__ uint64_t keys_seen(uint64_t sees, int off) {
+  const uint64_t up = off < 64 ? sees >> (off & 63) : 0ull;
+  const int n = -off;
+  const uint64_t down = n < 64 ? (sees << (n & 63)) | ((1ull << (n & 63)) - 1ull) : ~0ull;
+  return off >= 0 ? up : down;
+}
+
+template <int RB, int D>
+struct Wave8 {
+  bf16x8 q[RB][D / 32];
+  f32x4 o[RB][D / 16];
+  float m[RB], l[RB];  // reference maximum of the unscaled scores (kNegBig: no key seen yet), sum
+  uint64_t sees[RB];   // of the step's own positions
+  uint32_t nan;        // a NaN code was left out of O
+};
+
+// Scores of one 64-key block less `base`: the accumulators start there, so that
+// the difference that the exponential takes costs no instruction and keeps its
+// bits however large the scores are.  MASKED: some key lies past `first`, the
+// first of the step's positions; what a row does not see is -inf.
+template <int RB, int D, bool MASKED>
+__device__ __forceinline__ void block_scores(const Wave8<RB, D>& w, const u32x4 (&kr)[4][D / 64], float ks, int off,
+                                             const float (&base)[RB], f32x4 (&sc)[RB][4]) {
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) sc[rb][t] = f32x4{base[rb], base[rb], base[rb], base[rb]};
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const bf16x8 kf = widen8(kr[t][i][2 * h], kr[t][i][2 * h + 1], ks);
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) sc[rb][t] = mfma16x16x32(kf, w.q[rb][2 * i + h], sc[rb][t]);
+      }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  if (MASKED) {
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      const uint64_t win = keys_seen(w.sees[rb], off);
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const uint32_t see = (uint32_t)(win >> (16 * t + r)) & 1u;
+          const uint32_t x = __float_as_uint(sc[rb][t][r]);
+          sc[rb][t][r] = __uint_as_float(see ? x : 0xff800000u);
+        }
+    }
+  }
+}
+
+// Each row's largest score of the block.
+template <int RB>
+__device__ __forceinline__ void block_max(const f32x4 (&sc)[RB][4], float (&mx)[RB]) {
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    float x = fmaxf(fmaxf(sc[rb][0][0], sc[rb][0][1]), fmaxf(sc[rb][0][2], sc[rb][0][3]));
+#pragma unroll
+    for (int t = 1; t < 4; ++t)
+      x = fmaxf(fmaxf(fmaxf(x, sc[rb][t][0]), sc[rb][t][1]), fmaxf(sc[rb][t][2], sc[rb][t][3]));
+    mx[rb] = max_over_groups(x);
+  }
+}
+
+// Folds one block into O and the sums; false, and nothing folded, when some
+// row's maximum has outgrown its reference.  load_k and load_v fetch the next
+// block once kr and vr are free.
+template <int RB, int D, bool MASKED, typename LoadK, typename LoadV>
+__device__ __forceinline__ bool fold_block(Wave8<RB, D>& w, u32x4 (&kr)[4][D / 64], u32x4 (&vr)[D / 16], float ks,
+                                           float vs, float scale_log2, int key0, int first, int end, LoadK load_k,
+                                           LoadV load_v) {
+  const int lg = (threadIdx.x & 63) >> 4;
+  f32x4 sc[RB][4];
+  float base[RB], mx[RB];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) base[rb] = w.m[rb] > kNegBig ? -w.m[rb] : 0.f;
+  block_scores<RB, D, MASKED>(w, kr, ks, key0 + 4 * lg - first, base, sc);
+  load_k();
+  block_max<RB>(sc, mx);
+  bool grow = false;
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) grow |= mx[rb] * scale_log2 > (w.m[rb] > kNegBig ? kGrowLog2 : kNegBig);
+  if (__builtin_expect(__ballot(grow) != 0, 0)) return false;
+  // P in bfloat16, as the products take it; the sum adds the rounded values,
+  // so that the weights that O accumulates sum to one.
+  bf16x8 pf[RB][2];
+  const bf16x2 ones = {(__bf16)1.f, (__bf16)1.f};
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    float acc = w.l[rb];
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; r += 2) {
+        const f32x2 x = {__builtin_amdgcn_exp2f(sc[rb][t][r] * scale_log2),
+                         __builtin_amdgcn_exp2f(sc[rb][t][r + 1] * scale_log2)};
+        const bf16x2 pb = __builtin_convertvector(x, bf16x2);
+        pf[rb][t / 2][(t & 1) * 4 + r] = pb[0];
+        pf[rb][t / 2][(t & 1) * 4 + r + 1] = pb[1];
+        acc = __builtin_amdgcn_fdot2_f32_bf16(pb, ones, acc, false);
+      }
+    w.l[rb] = acc;
+  }
+  if (MASKED) {
+    // What lies past the last key is not read as numbers, and NaN codes are
+    // left to spread_nan: 0 * NaN would reach the rows that do not see them.
+#pragma unroll
+    for (int db = 0; db < D / 16; ++db)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        vr[db][t] &= bytes_before(key0 + 16 * t + 4 * lg, end);
+        const uint32_t hit = nan_bytes(vr[db][t]);
+        w.nan |= hit;
+        vr[db][t] &= ~(hit * 0xffu);
+      }
+  }
+#pragma unroll
+  for (int db = 0; db < D / 16; ++db)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const bf16x8 vf = widen8(vr[db][2 * h], vr[db][2 * h + 1], vs);
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) w.o[rb][db] = mfma16x16x32(vf, pf[rb][h], w.o[rb][db]);
+      if (h == 1 && (db & 1)) __builtin_amdgcn_sched_barrier(0);
+    }
+  load_v();
+  return true;
+}
+
+// Makes the outputs NaN that a NaN code of this block reaches: those of the rows
+// that see its key, in its column.
+template <int RB, int D>
+__device__ __forceinline__ void spread_nan(Wave8<RB, D>& w, u32x4 (&vr)[D / 16], int key0, int first, int end) {
+  const int lg = (threadIdx.x & 63) >> 4;
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    const uint64_t win = keys_seen(w.sees[rb], key0 + 4 * lg - first);
+    bf16x8 sf[2];  // 1 where the row sees the key
+#pragma unroll
+    for (int j = 0; j < 16; ++j) sf[j >> 3][j & 7] = (__bf16)(float)((uint32_t)(win >> (16 * (j >> 2) + (j & 3))) & 1u);
+#pragma unroll
+    for (int db = 0; db < D / 16; ++db) {
+      u32x4 ind;  // 1 (code 0x38) where V is NaN
+#pragma unroll
+      for (int t = 0; t < 4; ++t) ind[t] = nan_bytes(vr[db][t] & bytes_before(key0 + 16 * t + 4 * lg, end)) * 0x38u;
+      f32x4 n = {0.f, 0.f, 0.f, 0.f};
+      n = mfma16x16x32(widen8(ind[0], ind[1], 1.f), sf[0], n);
+      n = mfma16x16x32(widen8(ind[2], ind[3], 1.f), sf[1], n);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        w.o[rb][db][e] = __uint_as_float(n[e] > 0.f ? 0x7fc00000u : __float_as_uint(w.o[rb][db][e]));
+    }
+  }
+}
+
+template <int RB, int D>
+__global__ __launch_bounds__(kItems * kWave, (RB <= 2 ? 2 : 1))
+void kv8_attn_kernel(AttnShape s, AttnBatch bt, Kv8Pool pool, int nitems, const uint16_t* __restrict__ q,
+                     AttnPartials parts) {
+  const int lane = threadIdx.x & 63;
+  const int lr = lane & 15, lg = lane >> 4;
+  const int item = __builtin_amdgcn_readfirstlane(blockIdx.x * kItems + (threadIdx.x >> 6));
+  if (item >= nitems) return;
+  // Row groups of one (chunk, KV head) are neighbours: their second reads of a block hit cache.
+  const int rg = item % s.row_groups;
+  const int head = item / s.row_groups % s.Hkv;
+  const int c = item / s.row_groups / s.Hkv;
+  int lo = 0, hi = bt.nreq - 1;  // the largest request with chunk_prefix <= c
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (bt.chunk_prefix[mid] <= c) lo = mid; else hi = mid - 1;
+  }
+  const int req = bt.req0 + lo;
+  const int end = bt.kv_len[lo], first = end - s.G;
+  const int key_begin = (c - bt.chunk_prefix[lo]) * s.chunk_keys;
+  const int key_end = min(key_begin + s.chunk_keys, end);
+  const int ntiles = (key_end - key_begin + kKeyBlock - 1) / kKeyBlock;
+  const int blk0 = key_begin / kKeyBlock;
+
+  // Lane j: where block j of the chunk lies, and its scales.
+  const int shift = pool.page_shift - 6;
+  const int blk = blk0 + min(lane, ntiles - 1);
+  int page = pool.table[(int64_t)req * pool.max_pages + (blk >> shift)];
+  page = min(max(page, 0), pool.num_pages - 1);
+  const int64_t at = (((int64_t)page * s.Hkv + head) << shift) + (blk & ((1 << shift) - 1));
+  const uint32_t at_lo = (uint32_t)at, at_hi = (uint32_t)(at >> 32);
+  const int ks_all = pool.k_scale[at], vs_all = pool.v_scale[at];
+
+  u32x4 kr[4][D / 64], vr[D / 16];
+  auto tile_at = [&](int t) {
+    return (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)at_hi, t) << 32) |
+                     (uint32_t)__builtin_amdgcn_readlane((int)at_lo, t)) * (D * kKeyBlock);
+  };
+  auto load_k = [&](int t) {
+    const uint8_t* p = pool.k + tile_at(min(t, ntiles - 1));
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) kr[j][i] = load_u32x4_stream(p + (i * 4 + j) * 1024 + lane * 16);
+  };
+  auto load_v = [&](int t) {
+    const uint8_t* p = pool.v + tile_at(min(t, ntiles - 1));
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) vr[i] = load_u32x4_stream(p + i * 1024 + lane * 16);
+  };
+  load_k(0);
+  load_v(0);
+
+  Wave8<RB, D> w;
+  const uint64_t masks = position_mask(bt.parent != nullptr ? bt.parent + (int64_t)req * (s.G - 1) : nullptr, s.G);
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    const int row = (rg * RB + rb) * 16 + lr;
+    const int rc = min(row, s.rows - 1);
+    const int j = rc / s.group, h = head * s.group + rc - j * s.group;
+    const uint16_t* src = q + (((int64_t)req * s.G + j) * s.Hq + h) * D + 16 * lg;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) w.q[rb][i] = load_bf16x8(src + 64 * (i >> 1) + 8 * (i & 1));
+    const uint32_t a = __shfl((uint32_t)masks, j), b = __shfl((uint32_t)(masks >> 32), j);
+    w.sees[rb] = ((uint64_t)b << 32) | a;
+    w.m[rb] = kNegBig;
+  }
+
+  auto pow2 = [&](int bytes, int t) {
+    return __uint_as_float((uint32_t)__builtin_amdgcn_readlane(bytes, t) << 23);
+  };
+  const int whole = min(max((first + 1 - key_begin) / kKeyBlock, 0), ntiles);  // blocks that every row sees whole
+  int from = 0, to = 1;  // blocks whose maxima are taken before the next fold
+  for (;;) {
+    for (int t = from; t < to; ++t) {
+      if (t > 0) load_k(t);
+      f32x4 sc[RB][4];
+      float zero[RB], mx[RB];
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) zero[rb] = 0.f;
+      block_scores<RB, D, true>(w, kr, pow2(ks_all, t), key_begin + t * kKeyBlock + 4 * lg - first, zero, sc);
+      block_max<RB>(sc, mx);
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) w.m[rb] = fmaxf(w.m[rb], mx[rb]);
+    }
+    if (from > 0) {
+      load_k(0);
+      load_v(0);
+    }
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      w.l[rb] = 0.f;
+#pragma unroll
+      for (int db = 0; db < D / 16; ++db) w.o[rb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    // Two loops: in one, the compiler widens the codes before it branches to
+    // either kind of block, and spills what that takes.
+    w.nan = 0;
+    int t = 0;
+    bool done = true;
+    for (; t < whole && done; ++t)
+      done = fold_block<RB, D, false>(w, kr, vr, pow2(ks_all, t), pow2(vs_all, t), s.scale_log2, 0, 0, 0,
+                                      [&] { load_k(t + 1); }, [&] { load_v(t + 1); });
+    for (; t < ntiles && done; ++t)
+      done = fold_block<RB, D, true>(w, kr, vr, pow2(ks_all, t), pow2(vs_all, t), s.scale_log2,
+                                     key_begin + t * kKeyBlock, first, end, [&] { load_k(t + 1); }, [&] { load_v(t + 1); });
+    if (done) break;
+    from = t - 1;
+    to = ntiles;
+  }
+
+  if (__builtin_expect(__ballot(w.nan != 0) != 0, 0)) {
+    for (int t = whole; t < ntiles; ++t) {
+      load_v(t);
+      spread_nan<RB, D>(w, vr, key_begin + t * kKeyBlock, first, end);
+    }
+  }
+
+  const int64_t slot = (int64_t)(bt.chunk_base + c) * s.Hkv + head;
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    const int row = (rg * RB + rb) * 16 + lr;
+    const float l = sum_over_groups(w.l[rb]);
+    if (row < s.rows) {
+      if (lg == 0) {
+        parts.m[slot * s.rows + row] = w.m[rb];
+        parts.l[slot * s.rows + row] = l;
+      }
+      float* dst = parts.o + (slot * s.rows + row) * D + 4 * lg;
+#pragma unroll
+      for (int db = 0; db < D / 16; ++db) *reinterpret_cast<f32x4*>(dst + db * 16) = w.o[rb][db];
+    }
+  }
+}
+
+// Joins the partials of each (request, position, head) in chunk order: O =
+// sum_c w_c o_c / sum_c w_c l_c, w_c = 2^(scale_log2 (m_c - max m)).  A thread
+// holds four columns.
+template <int D>
+__global__ __launch_bounds__(256)
+void kv8_merge_kernel(AttnShape s, AttnBatch bt, AttnPartials parts, uint16_t* __restrict__ out) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i >= s.rows * (D / 4)) return;
+  const int head = blockIdx.y, b = blockIdx.z;
+  const int row = i / (D / 4), d = i % (D / 4) * 4;
+  const int c0 = bt.chunk_base + bt.chunk_prefix[b], c1 = bt.chunk_base + bt.chunk_prefix[b + 1];
+  constexpr int kN = 8;  // chunks in flight
+  float m = kNegBig, den = 0.f;
+  f32x4 num = {0.f, 0.f, 0.f, 0.f};
+  for (int c = c0; c < c1; c += kN) {
+    float mc[kN], lc[kN];
+    f32x4 oc[kN];
+#pragma unroll
+    for (int k = 0; k < kN; ++k) {
+      const int64_t at = ((int64_t)min(c + k, c1 - 1) * s.Hkv + head) * s.rows + row;
+      mc[k] = parts.m[at];
+      lc[k] = parts.l[at];
+      oc[k] = *reinterpret_cast<const f32x4*>(parts.o + at * D + d);
+    }
+    float mn = m;
+#pragma unroll
+    for (int k = 0; k < kN; ++k) mn = fmaxf(mn, mc[k]);
+    const float alpha = __builtin_amdgcn_exp2f((m - mn) * s.scale_log2);
+    den *= alpha;
+    num *= alpha;
+#pragma unroll
+    for (int k = 0; k < kN; ++k)
+      if (c + k < c1) {
+        const float a = __builtin_amdgcn_exp2f((mc[k] - mn) * s.scale_log2);
+        den = fmaf(a, lc[k], den);
+        num += a * oc[k];
+      }
+    m = mn;
+  }
+  const int j = row / s.group, h = head * s.group + row - j * s.group;
+  uint16_t* dst = out + (((int64_t)(bt.req0 + b) * s.G + j) * s.Hq + h) * D + d;
+  const float r = 1.f / den;
+  const bf16x2 lo = __builtin_convertvector((f32x2{num[0] * r, num[1] * r}), bf16x2);
+  const bf16x2 hi = __builtin_convertvector((f32x2{num[2] * r, num[3] * r}), bf16x2);
+  *reinterpret_cast<u32x2*>(dst) = u32x2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+}
+
+int64_t cu_count() {
+  static std::atomic<int> cached[64];
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return 256;
+  int n = cached[dev].load(std::memory_order_relaxed);
+  if (n <= 0) {
+    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n <= 0) n = 256;
+    cached[dev].store(n, std::memory_order_relaxed);
+  }
+  return n;
+}
+
+int row_groups(int rows) {
+  const int blocks = (rows + 15) / 16;
+  return (blocks + kMaxBlocks - 1) / kMaxBlocks;
+}
+int blocks_per_wave(int rows) {
+  const int g = row_groups(rows);
+  return ((rows + 15) / 16 + g - 1) / g;
+}
+
+// Chunk lengths, in 64-key blocks.
+constexpr int kChunks[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 64};
+constexpr int kNumChunks = sizeof(kChunks) / sizeof(kChunks[0]);
+static_assert(kChunks[kNumChunks - 1] == kMaxTiles, "the longest chunk fills a wave's lanes");
+
+}  // namespace
+
+AttnShape kv8_shape(int G, int Hq, int Hkv, int D, float scale, const int32_t* kv_len, int B) {
+  AttnShape s;
+  s.G = G;
+  s.Hq = Hq;
+  s.Hkv = Hkv;
+  s.D = D;
+  s.group = Hq / Hkv;
+  s.rows = G * s.group;
+  s.row_groups = row_groups(s.rows);
+  s.scale_log2 = scale * kLog2e;
+  // Rounds of items over the wave slots, times an item's length with its
+  // start-up (rows, pages, first block, partial; in keys).
+  const int64_t per_chunk = (int64_t)Hkv * s.row_groups;
+  const int64_t slots = cu_count() * (blocks_per_wave(s.rows) <= 2 ? 8 : 4);
+  const int64_t start = 192 + 2 * s.rows;
+  int64_t best = INT64_MAX;
+  s.chunk_keys = kMaxTiles * kKeyBlock;
+  for (int i = kNumChunks - 1; i >= 0; --i) {
+    const int keys = kChunks[i] * kKeyBlock;
+    int64_t chunks = 0;
+    for (int b = 0; b < B; ++b) chunks += (kv_len[b] + keys - 1) / keys;
+    const int64_t items = chunks * per_chunk;
+    if (items > 4 * slots && i < kNumChunks - 1) break;  // shorter chunks: more partials than the workspace holds
+    const int64_t cost = (items + slots - 1) / slots * (keys + start);
+    if (cost < best) {
+      best = cost;
+      s.chunk_keys = keys;
+    }
+  }
+  return s;
+}
+
+int64_t kv8_max_chunks(int G, int Hq, int Hkv, int D, int B, int64_t max_kv_len) {
+  (void)D;
+  const int rows = G * (Hq / Hkv);
+  const int64_t slots = cu_count() * (blocks_per_wave(rows) <= 2 ? 8 : 4);
+  const int64_t most = 4 * slots / ((int64_t)Hkv * row_groups(rows));
+  const int64_t at_longest = B * ((max_kv_len + kMaxTiles * kKeyBlock - 1) / (kMaxTiles * kKeyBlock));
+  return most > at_longest ? most : at_longest;
+}
+
+hipError_t launch_kv8_attention(const AttnShape& s, const AttnBatch& batch, const Kv8Pool& pool, int nchunks,
+                                const void* q, AttnPartials parts, void* out, hipStream_t stream) {
+  const int nitems = nchunks * s.Hkv * s.row_groups;
+  const dim3 grid((nitems + kItems - 1) / kItems), block(kItems * kWave);
+#define SDV_KV8(RB)                                                                                          \
+  case RB:                                                                                                   \
+    if (s.D == 128)                                                                                          \
+      hipLaunchKernelGGL((kv8_attn_kernel<RB, 128>), grid, block, 0, stream, s, batch, pool, nitems,          \
+                         static_cast<const uint16_t*>(q), parts);                                            \
+    else                                                                                                     \
+      hipLaunchKernelGGL((kv8_attn_kernel<RB, 64>), grid, block, 0, stream, s, batch, pool, nitems,           \
+                         static_cast<const uint16_t*>(q), parts);                                            \
+    break;
+  switch (blocks_per_wave(s.rows)) {
+    SDV_KV8(1) SDV_KV8(2) SDV_KV8(3) SDV_KV8(4) SDV_KV8(5)
+    default: return hipErrorInvalidValue;
+  }
+#undef SDV_KV8
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const dim3 mgrid((s.rows * (s.D / 4) + 255) / 256, s.Hkv, batch.nreq);
+  if (s.D == 128)
+    hipLaunchKernelGGL(kv8_merge_kernel<128>, mgrid, dim3(256), 0, stream, s, batch, parts, static_cast<uint16_t*>(out));
+  else
+    hipLaunchKernelGGL(kv8_merge_kernel<64>, mgrid, dim3(256), 0, stream, s, batch, parts, static_cast<uint16_t*>(out));
+  return hipGetLastError();
+}
+
+}  // namespace sdv

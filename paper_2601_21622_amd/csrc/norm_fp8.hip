@@ -1,0 +1,151 @@
+// Residual addition, root-mean-square norm and 8-bit output (gfx950).
+//
+//   h = x + residual,  y = h * weight / sqrt(mean(h^2) + eps),
+//   per 128 columns: s = max(max|y| / 448, 2^-126), code = e4m3(y / s).
+//
+// One workgroup per row: a thread holds R groups of eight columns in registers,
+// so that the row is read once; 16 lanes hold the 128 columns of a scale.  Bound
+// by memory: bf16 rows read 4 bytes and write 3 per column.  Squares are summed
+// in float64: float32 squares of values past 1.8e19 overflow, and the
+// conversions hide behind the loads.
+#include "fp8.h"
+
+namespace sdv {
+
+namespace {
+
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, float (&v)[8]);
+template <>
+__device__ __forceinline__ void load8<uint16_t>(const uint16_t* p, float (&v)[8]) {
+  const u32x4 r = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = __uint_as_float(r[i] << 16);
+    v[2 * i + 1] = __uint_as_float(r[i] & 0xffff0000u);
+  }
+}
+template <>
+__device__ __forceinline__ void load8<float>(const float* p, float (&v)[8]) {
+  const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[i] = a[i];
+    v[4 + i] = b[i];
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store8(T* p, const float (&v)[8]);
+template <>
+__device__ __forceinline__ void store8<uint16_t>(uint16_t* p, const float (&v)[8]) {
+  bf16x8 r;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) r[i] = (__bf16)v[i];
+  *reinterpret_cast<u32x4*>(p) = __builtin_bit_cast(u32x4, r);
+}
+template <>
+__device__ __forceinline__ void store8<float>(float* p, const float (&v)[8]) {
+  *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
+  *reinterpret_cast<f32x4*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+}
+
+// Maximum over the 16 lanes of a DPP row.
+__device__ __forceinline__ float row_max(float v) {
+  v = fmaxf(v, dpp_f32<kDppXor1>(v));
+  v = fmaxf(v, dpp_f32<kDppXor2>(v));
+  v = fmaxf(v, dpp_f32<kDppRowHalfMirror>(v));
+  return fmaxf(v, dpp_f32<kDppRowMirror>(v));
+}
+
+template <typename T, int THREADS, int R>
+__global__ __launch_bounds__(THREADS)
+void residual_norm_kernel(int rows, int width, float eps, const T* x, const T* residual, const T* __restrict__ weight,
+                          T* new_residual, uint8_t* __restrict__ out, float* __restrict__ out_scale) {
+  constexpr int NW = THREADS / kWave;
+  __shared__ double part[NW];
+  const int row = blockIdx.x, t = threadIdx.x;
+  const int groups = width / 8;
+  const int64_t base = (int64_t)row * width;
+  float h[R][8];
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const int g = min(t + i * THREADS, groups - 1);  // lanes past the row read its last group, unused
+    load8(x + base + g * 8, h[i]);
+  }
+  if (residual != nullptr) {
+    float r[R][8];
+#pragma unroll
+    for (int i = 0; i < R; ++i) load8(residual + base + min(t + i * THREADS, groups - 1) * 8, r[i]);
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) h[i][e] += r[i][e];
+  }
+  double sum = 0.0;
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+    if (t + i * THREADS < groups) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum = fma((double)h[i][e], (double)h[i][e], sum);
+    }
+  sum = wave_sum_f64(sum);
+  if (NW > 1) {
+    if ((t & 63) == 0) part[t >> 6] = sum;
+    __syncthreads();
+    sum = part[0];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) sum += part[w];
+  }
+  const float inv = (float)(1.0 / sqrt(sum / (double)width + (double)eps));
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const int g = t + i * THREADS;
+    const bool live = g < groups;
+    if (live && new_residual != nullptr) store8(new_residual + base + g * 8, h[i]);
+    float w[8], y[8], most = 0.f;
+    load8(weight + min(g, groups - 1) * 8, w);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      y[e] = h[i][e] * inv * w[e];
+      most = fmaxf(most, live ? fabsf(y[e]) : 0.f);
+    }
+    most = row_max(most);
+    const float s = fmaxf(most / 448.f, 0x1p-126f);
+    const float to = 1.f / s;
+    if (live) {
+      const u32x2 c = {encode4(y[0] * to, y[1] * to, y[2] * to, y[3] * to),
+                       encode4(y[4] * to, y[5] * to, y[6] * to, y[7] * to)};
+      *reinterpret_cast<u32x2*>(out + base + g * 8) = c;
+      if ((t & 15) == 0) out_scale[(int64_t)(g / 16) * rows + row] = s;
+    }
+  }
+}
+
+}  // namespace
+
+hipError_t launch_residual_norm(bool f32, int rows, int width, float eps, const void* x, const void* residual,
+                                const void* weight, void* new_residual, uint8_t* out, float* out_scale,
+                                hipStream_t stream) {
+  const int groups = width / 8;
+#define SDV_NORM(T, N, R)                                                                                             \
+  hipLaunchKernelGGL((residual_norm_kernel<T, N, R>), dim3(rows), dim3(N), 0, stream, rows, width, eps,               \
+                     static_cast<const T*>(x), static_cast<const T*>(residual), static_cast<const T*>(weight),        \
+                     static_cast<T*>(new_residual), out, out_scale)
+#define SDV_NORM_SIZES(T)                            \
+  if (groups <= 64) SDV_NORM(T, 64, 1);              \
+  else if (groups <= 256) SDV_NORM(T, 256, 1);       \
+  else if (groups <= 512) SDV_NORM(T, 256, 2);       \
+  else if (groups <= 1024) SDV_NORM(T, 256, 4);      \
+  else if (groups <= 2048) SDV_NORM(T, 1024, 2);     \
+  else SDV_NORM(T, 1024, 4);
+  if (f32) {
+    SDV_NORM_SIZES(float)
+  } else {
+    SDV_NORM_SIZES(uint16_t)
+  }
+#undef SDV_NORM_SIZES
+#undef SDV_NORM
+  return hipGetLastError();
+}
+
+}  // namespace sdv

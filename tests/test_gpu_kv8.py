@@ -1,0 +1,339 @@
+"""The 8-bit KV cache on the GPU against the float64 oracle: appends code for
+code, attention within a bound that is derived in check_attention."""
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2601_21622_amd as sd
+from oracle import fp8, tree_attention, verify_attention
+
+from gpu_util import announce
+
+pytestmark = pytest.mark.gpu
+
+F8 = torch.float8_e4m3fn
+
+
+def make_table(rng, kv_len, page, spare=2):
+    need = [-(-int(n) // page) for n in kv_len]
+    n = sum(need) + spare
+    ids = iter(rng.permutation(n).tolist())
+    table = np.full((len(kv_len), max(1, max(need))), -1, dtype=np.int32)
+    for j in range(table.shape[1]):
+        for b in range(len(kv_len)):
+            if j < need[b]:
+                table[b, j] = next(ids)
+    return table, n
+
+
+class Cache:
+    """A pool on both sides, its bytes seeded (codes of any kind, NaN among them)."""
+
+    def __init__(self, rng, kv_len, heads, dim, page, batch=None):
+        self.dim, self.page = dim, page
+        self.table, n = make_table(rng, kv_len, page)
+        shape = (n, heads, page // 64)
+        self.k, self.v = (rng.integers(0, 256, (*shape, 64 * dim), dtype=np.uint8) for _ in range(2))
+        self.ks, self.vs = (rng.integers(115, 125, shape, dtype=np.uint8) for _ in range(2))
+        self.dev = [torch.from_numpy(a.copy()).cuda() for a in (self.k, self.v, self.ks, self.vs)]
+        self.handle = sd.KV8Cache.of(self.dev[0].view(n, heads, page // 64, 64 * dim), *self.dev[1:],
+                                     torch.from_numpy(self.table).cuda(), page)
+
+    def upload(self):
+        for d, a in zip(self.dev, (self.k, self.v, self.ks, self.vs)):
+            d.copy_(torch.from_numpy(a))
+
+    def append(self, k_new, v_new, off, new, lens):
+        self.k, self.ks = fp8.append(self.k, self.ks, self.table, k_new, off, new, lens, fp8.k_index(self.dim))
+        self.v, self.vs = fp8.append(self.v, self.vs, self.table, v_new, off, new, lens, fp8.v_index(self.dim))
+
+    def check(self):
+        for name, d, a in zip(("k", "v", "k_scale", "v_scale"), self.dev, (self.k, self.v, self.ks, self.vs)):
+            got = d.cpu().numpy()
+            if name in ("k", "v"):  # one NaN is as good as another
+                got, a = (np.where(x & 127 == 127, 127, x) for x in (got, a))
+            assert np.array_equal(got, a), f"{name}: {(got != a).sum()} of {a.size} differ"
+
+
+def rows(rng, total, heads, dim, dtype, stride=None):
+    """Token rows (magnitudes differ by head and row) on the GPU, and their exact values."""
+    x = rng.normal(size=(total, heads, dim)) * 2.0 ** rng.integers(-12, 12, (1, heads, 1)) * 2.0 ** rng.integers(-2, 3, (total, 1, 1))
+    full = torch.zeros((max(total, 1), stride or heads * dim), dtype=dtype)
+    view = full[:, :heads * dim].unflatten(1, (heads, dim))
+    view[:total] = torch.from_numpy(x).to(dtype)
+    dev = full.cuda()[:, :heads * dim].unflatten(1, (heads, dim))
+    return dev, view[:total].double().numpy()
+
+
+APPENDS = {
+    # name: heads, dim, page, dtype, stride, [(new, kv) per request]
+    "one_row_each": (2, 128, 64, torch.bfloat16, None, [(1, 1), (1, 64), (1, 65), (1, 128), (1, 100)]),
+    "step_over_pages": (4, 128, 64, torch.bfloat16, None, [(5, 5), (5, 66), (5, 130), (5, 64)]),
+    "prompts": (2, 128, 256, torch.bfloat16, 3 * 256, [(300, 300), (64, 64), (1, 1), (0, 0), (513, 600)]),
+    "d64": (3, 64, 128, torch.bfloat16, None, [(7, 60), (200, 200), (64, 128), (0, 50)]),
+    "f32": (2, 128, 64, torch.float32, 264, [(70, 75), (3, 130)]),
+    "f32_d64": (1, 64, 4096, torch.float32, None, [(130, 4000), (2, 64)]),
+    "many": (1, 64, 64, torch.bfloat16, None, [(1 + i % 3, 4 + 5 * i) for i in range(70)]),
+    "whole_blocks": (1, 128, 128, torch.bfloat16, None, [(128, 256), (64, 128)]),
+}
+
+
+@pytest.mark.parametrize("name", APPENDS)
+def test_append(name):
+    heads, dim, page, dtype, stride, req = APPENDS[name]
+    rng = np.random.default_rng(len(name))
+    new, lens = [a for a, _ in req], [b for _, b in req]
+    c = Cache(rng, lens, heads, dim, page)
+    off = np.cumsum([0] + new[:-1])
+    (kd, kx), (vd, vx) = rows(rng, sum(new), heads, dim, dtype, stride), rows(rng, sum(new), heads, dim, dtype, stride)
+    d = sd.Dims(len(req), 0, heads, heads, dim, 32, 1, 1 if dtype == torch.bfloat16 else 0, 0)
+    for _ in range(2):  # a second time changes nothing but rows that the first rescaled once
+        c.append(kx, vx, off, new, lens)
+        sd.sd_kv8_append(d, c.handle, kd, vd, off, new, lens)
+        torch.cuda.synchronize()
+        c.check()
+
+
+def test_append_steps_cut_back_and_odd_values():
+    """A session's life: prompt, steps, a cut back to fewer keys, rows of
+    zeros, infinities, NaN, the largest and smallest numbers; rows shared by requests."""
+    rng = np.random.default_rng(5)
+    heads, dim = 2, 64
+    c = Cache(rng, [200, 200], heads, dim, 64)
+    d = sd.Dims(2, 0, heads, heads, dim, 32, 1, 0, 0)
+    for new, lens in (([90, 3], [90, 3]), ([5, 5], [95, 8]), ([5, 5], [97, 10]), ([1, 60], [98, 66]), ([30, 0], [120, 66]),
+                      ([64, 1], [192, 1])):
+        (kd, kx), (vd, vx) = rows(rng, 100, heads, dim, torch.float32), rows(rng, 100, heads, dim, torch.float32)
+        for dev, x in ((kd, kx), (vd, vx)):
+            odd = [0.0, -0.0, np.inf, -np.inf, np.nan, 3.4e38, -3.4e38, 1e-45, 1e-38]
+            at = rng.integers(0, 100, len(odd)), rng.integers(0, heads, len(odd)), rng.integers(0, dim, len(odd))
+            x[at] = np.float32(odd)
+            x[7] = 0.0
+            dev.copy_(torch.from_numpy(x.astype(np.float32)))
+        off = [3, 3]  # both requests read the same rows
+        c.append(kx, vx, off, new, lens)
+        sd.sd_kv8_append(d, c.handle, kd, vd, off, new, lens)
+        torch.cuda.synchronize()
+        c.check()
+
+
+# ---- attention -------------------------------------------------------------------
+
+def check_attention(got, q, seg, kv_len, heads, parent, scale, what):
+    """Bound: P is rounded to bf16 (half a step: 2^-8) where it is multiplied, and
+    the sum that divides adds the rounded values, so |O - O*| <= 2^-8 (A + |O*|), A = sum p |v|;
+    the output's own rounding adds 2^-8 |O|.  Scores are float32 sums of D exact products: a
+    relative error of p of at most D 2^-24 |q| |k| scale and a few 2^-24 of |s|, which with the
+    second-order terms is held within a twentieth of the bound for the scores used here (< 40)."""
+    kseg, vseg, off = seg
+    f = verify_attention if parent is None else lambda *a: tree_attention(*a[:-1], parent, a[-1])
+    ref = f(q, kseg, vseg, off, kv_len, heads, scale)
+    mag = f(q, kseg, np.abs(vseg), off, kv_len, heads, scale)
+    bound = 1.05 * 2.0 ** -8 * (mag + 2 * np.abs(ref)) + 1e-30
+    err = np.abs(got - ref)
+    bad = ~(err <= bound)
+    assert not bad.any(), f"{what}: {bad.sum()} of {bad.size} past the bound, first {np.argwhere(bad)[0]}"
+    return float((err / bound).max())
+
+
+ATTENDS = {
+    # name: G, Hq, Hkv, D, page, lens, tree
+    "single_token": (1, 8, 2, 128, 64, [1, 64, 65, 300], False),
+    "single_token_mha": (1, 2, 2, 64, 64, [1, 2, 129], False),
+    "mha": (5, 3, 3, 128, 64, [5, 64, 66, 68, 700], False),
+    "gqa4": (7, 8, 2, 128, 128, [7, 63, 64, 65, 71, 1100], False),
+    "gqa8_72": (9, 16, 2, 128, 256, [9, 130, 1500], False),
+    "rows48_d64": (6, 16, 2, 64, 64, [6, 62, 128, 500], False),
+    "rows64": (8, 8, 1, 128, 64, [8, 200], False),
+    "rows88_two_groups": (11, 8, 1, 128, 64, [11, 300], False),
+    "rows128": (16, 8, 1, 128, 4096, [16, 5000], False),
+    "rows128_d64": (64, 4, 2, 64, 64, [64, 65, 127, 400], False),
+    "g64": (64, 1, 1, 128, 64, [64, 191], False),
+    "tree15": (16, 6, 2, 64, 128, [16, 37, 200, 801], True),
+    "tree63": (64, 2, 1, 128, 64, [64, 100, 130], True),
+    "many_requests": (2, 2, 2, 64, 64, [2 + 7 * i for i in range(70)], False),
+}
+
+
+def attend(G, Hq, Hkv, D, c, kv_len, q, parent, scale):
+    B = len(kv_len)
+    d = sd.Dims(B, G - 1, Hq, Hkv, D, 32, 1, 1, 0)
+    ws = torch.full((sd.sd_fp8_workspace_bytes(d, max(kv_len)),), 0xff, dtype=torch.uint8, device="cuda")
+    out = torch.full((B, G, Hq, D), float("nan"), dtype=torch.bfloat16, device="cuda")
+    sd.sd_verify_attention_kv8(d, q, c.handle, kv_len, parent, scale, out, ws)
+    torch.cuda.synchronize()
+    return out.double().cpu().numpy()
+
+
+def filled(rng, kv_len, heads, dim, page):
+    """A cache whose keys up to kv_len hold numbers, all other bytes anything (NaN too)."""
+    c = Cache(rng, kv_len, heads, dim, page)
+    total = int(sum(kv_len))
+    x = [rng.normal(size=(total, heads, dim)) for _ in range(2)]
+    off = np.cumsum([0] + list(kv_len[:-1]))
+    c.append(*x, off, kv_len, kv_len)
+    c.upload()
+    return c
+
+
+@pytest.mark.parametrize("name", ATTENDS)
+def test_attention(name):
+    G, Hq, Hkv, D, page, lens, tree = ATTENDS[name]
+    rng = np.random.default_rng(100 + len(name))
+    c = filled(rng, lens, Hkv, D, page)
+    q = torch.from_numpy(rng.normal(size=(len(lens), G, Hq, D)) * 2).bfloat16()
+    parent = pd = None
+    if tree:
+        parent = np.maximum(np.arange(G - 1)[None, :] - rng.integers(1, 5, (len(lens), G - 1)), -1).astype(np.int32)
+        pd = torch.from_numpy(parent).cuda()
+    scale = 1 / np.sqrt(D)
+    got = attend(G, Hq, Hkv, D, c, lens, q.cuda(), pd, scale)
+    seg = fp8.kv8_segments(c.k, c.v, c.ks, c.vs, c.table, lens)
+    worst = check_attention(got, q.double().numpy(), seg, lens, Hkv, parent, scale, name)
+    announce(f"kv8 attention {name}: {worst:.2f} of the bound")
+
+
+def test_attention_of_large_and_growing_scores():
+    """Keys that grow along the cache: the running maximum moves many times."""
+    rng = np.random.default_rng(9)
+    lens, G, H, D = [900, 333], 3, 2, 128
+    c = Cache(rng, lens, H, D, 64)
+    x = [rng.normal(size=(sum(lens), H, D)) for _ in range(2)]
+    x[0] *= np.concatenate([np.linspace(0.01, 3, n) for n in lens])[:, None, None]
+    c.append(*x, [0, 900], lens, lens)
+    c.upload()
+    q = torch.from_numpy(rng.normal(size=(2, G, H, D)) * 2).bfloat16()
+    got = attend(G, H, H, D, c, lens, q.cuda(), None, 1 / np.sqrt(D))
+    check_attention(got, q.double().numpy(), fp8.kv8_segments(c.k, c.v, c.ks, c.vs, c.table, lens), lens, H, None,
+                    1 / np.sqrt(D), "growing scores")
+
+
+@pytest.mark.parametrize("G,Hq,Hkv,D", [(4, 2, 1, 128), (4, 1, 1, 64), (9, 8, 1, 128)])
+def test_nan_reaches_only_those_that_see_it(G, Hq, Hkv, D):
+    """A draft whose rows are NaN spoils the positions from it on, not those before."""
+    rng = np.random.default_rng(11)
+    for L in (G, 62 + G // 2, 130):
+        for which in (0, 1):
+            c = Cache(rng, [L], Hkv, D, 64)
+            x = [rng.normal(size=(L, Hkv, D)) for _ in range(2)]
+            x[which][L - G + 2] = np.nan
+            c.append(*x, [0], [L], [L])
+            c.upload()
+            q = torch.from_numpy(rng.normal(size=(1, G, Hq, D))).bfloat16()
+            got = attend(G, Hq, Hkv, D, c, [L], q.cuda(), None, 1 / np.sqrt(D))
+            assert np.isnan(got[0, 2:]).all()
+            x[which][L - G + 2] = 0.0
+            clean = Cache(rng, [L], Hkv, D, 64)
+            clean.append(*x, [0], [L], [L])
+            seg = fp8.kv8_segments(clean.k, clean.v, clean.ks, clean.vs, clean.table, [L])
+            ref = verify_attention(q.double().numpy(), *seg, [L], Hkv)
+            assert np.isfinite(got[0, :2]).all()
+            assert np.abs(got[0, :2] - ref[0, :2]).max() < 0.1 * np.abs(ref).max()
+
+
+def test_inactive_values_of_queries_and_extremes():
+    """NaN and infinite queries spoil their own rows alone; a score far below the rest weighs nothing."""
+    rng = np.random.default_rng(12)
+    c = filled(rng, [200], 1, 128, 64)
+    q = torch.from_numpy(rng.normal(size=(1, 4, 2, 128))).bfloat16()
+    clean = attend(4, 2, 1, 128, c, [200], q.cuda(), None, 0.1)
+    q[0, 1, 0, 5] = float("nan")
+    q[0, 2, 1, 7] = float("inf")
+    got = attend(4, 2, 1, 128, c, [200], q.cuda(), None, 0.1)
+    assert np.isnan(got[0, 1, 0]).all() and np.isnan(got[0, 2, 1]).all()
+    keep = np.ones((4, 2), dtype=bool)
+    keep[1, 0] = keep[2, 1] = False
+    assert np.array_equal(got[0][keep], clean[0][keep])
+    big = torch.zeros((1, 4, 2, 128), dtype=torch.bfloat16)
+    big[..., 0] = 2.0 ** 60
+    got = attend(4, 2, 1, 128, c, [200], big.cuda(), None, 1.0)
+    k, v, _ = fp8.kv8_segments(c.k, c.v, c.ks, c.vs, c.table, [200])
+    best = k.reshape(200, 128)[:197, 0].argmax()
+    if (k.reshape(200, 128)[:197, 0] == k.reshape(200, 128)[best, 0]).sum() == 1:
+        assert np.abs(got[0, 0, 0] - v.reshape(200, 128)[best]).max() <= 2.0 ** -7 * np.abs(v).max()
+
+
+def test_streams_graphs_and_workspaces():
+    """Append and attention captured once, replayed with other data between
+    eager calls; another stream than the current one."""
+    rng = np.random.default_rng(13)
+    lens, G, H, D = [70, 133], 3, 2, 128
+    c = filled(rng, lens, H, D, 64)
+    d, da = sd.Dims(2, G - 1, 2 * H, H, D, 32, 1, 1, 0), sd.Dims(2, 0, H, H, D, 32, 1, 1, 0)
+    new = torch.randn((2 * G, H, D), device="cuda").bfloat16()
+    q = torch.randn((2, G, 2 * H, D), device="cuda").bfloat16()
+    out = torch.empty_like(q)
+    n = sd.sd_fp8_workspace_bytes(d, max(lens))
+    ws = torch.empty((n,), dtype=torch.uint8, device="cuda")
+
+    def step(o, w, stream=None):
+        sd.sd_kv8_append(da, c.handle, new, new, [0, G], [G, G], lens, stream=stream)
+        sd.sd_verify_attention_kv8(d, q, c.handle, lens, None, 0.1, o, w, stream=stream)
+
+    step(out, ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(out, ws)
+    eager, ws2 = torch.empty_like(out), torch.empty_like(ws)
+    side = torch.cuda.Stream()
+    for i in range(4):
+        new.normal_()
+        q.normal_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        step(eager, ws2, stream=side if i % 2 else None)
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager)
+        assert torch.isfinite(out).all()
+
+
+def test_far_pages():
+    """A pool past 4 GB: pages beyond 32-bit byte offsets."""
+    rng = np.random.default_rng(14)
+    heads, dim, page = 8, 128, 4096
+    n = 1100  # 1100 * 8 * 4096 * 128 = 4.6 GB
+    k, v = (torch.zeros((n, heads, page // 64, 64 * dim), dtype=torch.uint8, device="cuda") for _ in range(2))
+    ks, vs = (torch.full((n, heads, page // 64), 127, dtype=torch.uint8, device="cuda") for _ in range(2))
+    table = torch.tensor([[1099, 1030]], dtype=torch.int32, device="cuda")
+    cache = sd.KV8Cache.of(k, v, ks, vs, table, page)
+    L = 4096 + 70
+    new = [torch.randn((L, heads, dim), device="cuda").bfloat16() for _ in range(2)]
+    sd.sd_kv8_append(sd.Dims(1, 0, heads, heads, dim, 32, 1, 1, 0), cache, *new, [0], [L], [L])
+    d = sd.Dims(1, 0, heads, heads, dim, 32, 1, 1, 0)
+    q = torch.randn((1, 1, heads, dim), device="cuda").bfloat16()
+    out = torch.empty_like(q)
+    ws = torch.empty((sd.sd_fp8_workspace_bytes(d, L),), dtype=torch.uint8, device="cuda")
+    sd.sd_verify_attention_kv8(d, q, cache, [L], None, dim ** -0.5, out, ws)
+    host = [t[[1099, 1030]].cpu().numpy() for t in (k, v, ks, vs)]
+    assert not k[1031:1099].any() and not k[:1030].any()
+    seg = fp8.kv8_segments(*host, np.array([[0, 1]]), [L])
+    check_attention(out.double().cpu().numpy(), q.double().cpu().numpy(), seg, [L], heads, None, dim ** -0.5, "far pages")
+    x = new[0].double().cpu().numpy()
+    got = seg[0].reshape(heads, L, dim).transpose(1, 0, 2)
+    assert np.abs(got - x).max() <= 2.0 ** -4 * np.abs(x).max()
+
+
+def test_binding_refuses_what_does_not_fit():
+    rng = np.random.default_rng(15)
+    c = filled(rng, [64], 2, 64, 64)
+    d = sd.Dims(1, 0, 2, 2, 64, 32, 1, 1, 0)
+    x = torch.zeros((1, 2, 64), dtype=torch.bfloat16, device="cuda")
+    q = torch.zeros((1, 1, 2, 64), dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty((1 << 20,), dtype=torch.uint8, device="cuda")
+    for bad in (lambda: sd.sd_kv8_append(d, c.handle, x, x, [0], [2], [64]),              # past the rows
+                lambda: sd.sd_kv8_append(d, c.handle, x.float(), x, [0], [1], [64]),
+                lambda: sd.sd_kv8_append(d, c.handle, x[:, :1], x, [0], [1], [64]),
+                lambda: sd.sd_kv8_append(d, c.handle, x, x, [0, 1], [1, 1], [64, 64]),
+                lambda: sd.sd_kv8_append(sd.Dims(1, 0, 2, 2, 128, 32, 1, 1, 0), c.handle, x, x, [0], [1], [64]),
+                lambda: sd.sd_verify_attention_kv8(d, q, c.handle, [64], None, 1.0, q.float(), ws),
+                lambda: sd.sd_verify_attention_kv8(d, q[..., :32], c.handle, [64], None, 1.0, q, ws),
+                lambda: sd.sd_verify_attention_kv8(d, q, c.handle, [64, 64], None, 1.0, q, ws),
+                lambda: sd.KV8Cache.of(c.dev[0], c.dev[1], c.dev[2], c.dev[3], c.handle._tensors[4], 128),
+                lambda: sd.KV8Cache.of(c.dev[0], c.dev[1], c.dev[2], c.dev[3], c.handle._tensors[4].long(), 64)):
+        with pytest.raises(ValueError):
+            bad()
+    with pytest.raises(sd.SdError):
+        sd.sd_verify_attention_kv8(d, q, c.handle, [65], None, 1.0, torch.empty_like(q), ws)
