@@ -141,7 +141,7 @@ SD_API int sd_residual_norm_fp8(const sd_norm_t* norm, const void* x, const void
  * sd_verify_logits with 8-bit rows and weights:
  *   logits[m][v] = sum_c hidden_scale[c][m] * w_scale[v/128][c] * sum_{k in block c} hidden[m][k] * w[v][k]
  * over the blocks c of 128 columns.
- *   dims     batch and gamma (M = B * G rows), hidden (a multiple of 32), vocab
+ *   dims     batch and gamma (M = B * G rows), hidden (a multiple of 32, at most 2^23), vocab
  *   hidden   [M][hidden] e4m3; hidden_scale [ceil(hidden/128)][M] float32
  *   w        [V][hidden] e4m3; w_scale [ceil(V/128)][ceil(hidden/128)] float32
  *   logits   [M][V] float32; row_lse [M] float32

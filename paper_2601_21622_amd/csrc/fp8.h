@@ -51,7 +51,7 @@ hipError_t launch_residual_norm(bool f32, int rows, int width, float eps, const 
 // The projection's tiles for M rows, K columns, V entries.
 struct Fp8Plan {
   int M, K, V;
-  int mb, nb;       // 32-row blocks per workgroup, 32-entry blocks per wave
+  int mb, nw;       // 32-row blocks and waves (of 32 entries each) per workgroup
   int mtiles, ntiles;
 };
 Fp8Plan fp8_plan(int M, int K, int V);

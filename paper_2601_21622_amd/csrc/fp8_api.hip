@@ -18,7 +18,8 @@ constexpr int kMaxRows = 128;  // G * (Hq / Hkv)
 constexpr int kMaxGamma = 63;
 constexpr int kMaxVocab = 2097152;
 constexpr int64_t kMaxKvLen = int64_t(1) << 30;
-constexpr int kMaxWidth = 32768;
+constexpr int kMaxWidth = 32768;   // of a normed row
+constexpr int kMaxHidden = 1 << 23;  // a tile of 256 rows within 32-bit offsets
 constexpr int64_t kMaxGrid = (int64_t(1) << 24) - 1;  // workgroups along x
 
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
@@ -44,7 +45,7 @@ int check_attention(const sd_dims_t* d) {
 int check_projection(const sd_dims_t* d) {
   if (d == nullptr || d->batch < 1 || d->gamma < 0 || d->hidden < 1 || d->vocab < 1 || d->flags != 0)
     return SD_ERR_INVALID_ARGUMENT;
-  if (d->hidden % 32 != 0 || d->vocab > kMaxVocab) return SD_ERR_UNSUPPORTED;
+  if (d->hidden % 32 != 0 || d->hidden > kMaxHidden || d->vocab > kMaxVocab) return SD_ERR_UNSUPPORTED;
   if (int64_t(d->batch) * (int64_t(d->gamma) + 1) > (int64_t(1) << 24)) return SD_ERR_UNSUPPORTED;
   return SD_OK;
 }

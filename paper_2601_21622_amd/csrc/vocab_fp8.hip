@@ -30,31 +30,47 @@ namespace sdv {
 
 namespace {
 
-constexpr int kWaves = 4;
 constexpr int kScaleBytes = 1024;  // a stage's row scales: 256 floats
 
-constexpr int stage_bytes(int mb, int nb) { return (4 * mb + 4 * kWaves * nb) * 1024 + kScaleBytes; }
-constexpr int stages(int mb, int nb) {
-  const int n = 160 * 1024 / stage_bytes(mb, nb);
+constexpr int stage_bytes(int mb, int nw) { return 4 * (mb + nw) * 1024 + kScaleBytes; }
+constexpr int stages(int mb, int nw) {
+  const int n = 160 * 1024 / stage_bytes(mb, nw);
   return n < 6 ? n : 6;
 }
 
-// LDS DMA of four bytes per lane (as line_dma: lane l to lds + 4 l).
-__device__ __forceinline__ void word_dma(const float* g, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" : : "s"(lds), "v"(g) : "m0", "memory");
+// LDS DMA of 16 (or 4) bytes per lane from base + off into LDS bytes lds + 16 l
+// (4 l), both bases wave-uniform; as line_dma otherwise.
+template <bool NT>
+__device__ __forceinline__ void base_dma(const void* base, uint32_t off, uint32_t lds) {
+  if (NT)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt"
+                 : : "s"(lds), "v"(off), "s"(base) : "m0", "memory");
+  else
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                 : : "s"(lds), "v"(off), "s"(base) : "m0", "memory");
+}
+__device__ __forceinline__ void base_dma_word(const void* base, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
+               : : "s"(lds), "v"(off), "s"(base) : "m0", "memory");
 }
 
-template <int MB, int NB>
-__global__ __launch_bounds__(kWaves * kWave, 1)
+template <bool X>
+struct Flag {
+  static constexpr bool value = X;
+};
+
+template <int MB, int NW>
+__global__ __launch_bounds__(NW * kWave, 1)
 void vocab_fp8_kernel(int M, int K, int V, int ntiles, int mtiles, const uint8_t* __restrict__ hidden,
                       const float* __restrict__ hidden_scale, const uint8_t* __restrict__ w,
                       const float* __restrict__ w_scale, float* __restrict__ logits, float2* __restrict__ partials) {
-  constexpr int NW = kWaves;
   constexpr int kHBlocks = 4 * MB;
-  constexpr int kStage = stage_bytes(MB, NB);
+  constexpr int kStage = stage_bytes(MB, NW);
   constexpr int kScaleAt = kStage - kScaleBytes;
-  constexpr int S = stages(MB, NB);
-  constexpr int kOps = MB + 4 * NB + 1;  // DMAs per wave and line
+  constexpr int S = stages(MB, NW);
+  constexpr int kHOps = (kHBlocks + NW - 1) / NW;  // hidden blocks per wave (past the last: the last again)
+  constexpr int kOps = 4 + kHOps + 1;              // DMAs per wave and line
+  constexpr int kSteps = 4 * MB;
   static_assert(S >= 2 && (S - 1) * kOps < 64, "two stages; vmcnt holds 6 bits");
   __shared__ __align__(1024) unsigned char lds[S * kStage];
 
@@ -65,159 +81,176 @@ void vocab_fp8_kernel(int M, int K, int V, int ntiles, int mtiles, const uint8_t
   const int m0 = ((blockIdx.x % grp) >> 3) * MB * 32;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
-  const int blk0 = (tile * NW + wave) * NB;
-  const int nlines = (K + kColBlock - 1) / kColBlock;
-  const int last_units = (K - (nlines - 1) * kColBlock) / 16;  // 2, 4, 6 or 8
+  const int blk0 = tile * NW + wave;
+  const int nlines = K / kColBlock, nscales = (K + kColBlock - 1) / kColBlock;
 
   // Lane l of block q of a group brings unit (l % 8) - r / 2 of row r = 8 q + l
-  // / 8.  Rows past V and past M repeat the last row; units past the last line's
-  // end repeat earlier ones and are not read.
+  // / 8.  Rows past V and past M repeat the last row.  Offsets count from the
+  // tile's first rows, and its 256 rows of K < 2^23 bytes fit 32 bits.
   auto unit = [&](int q) { return ((lane & 7) - 4 * (q & 1) - (lane >> 4)) & 7; };
-  const char* wsrc[NB][4];
+  const uint8_t* wbase = w + (int64_t)tile * NW * 32 * K;
+  const uint8_t* hbase = hidden + (int64_t)m0 * K;
+  uint32_t woff[4], hoff[kHOps];
 #pragma unroll
-  for (int nb = 0; nb < NB; ++nb)
+  for (int q = 0; q < 4; ++q)
+    woff[q] = (uint32_t)min(wave * 32 + 8 * q + (lane >> 3), V - 1 - tile * NW * 32) * (uint32_t)K + unit(q) * 16;
+  int hblk[kHOps];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int row = min((blk0 + nb) * 32 + 8 * q + (lane >> 3), V - 1);
-      wsrc[nb][q] = reinterpret_cast<const char*>(w + (int64_t)row * K) + unit(q) * 16;
-    }
-  const char* hsrc[MB];  // block `wave` of every 32-row group
-#pragma unroll
-  for (int mb = 0; mb < MB; ++mb) {
-    const int row = min(m0 + mb * 32 + 8 * wave + (lane >> 3), M - 1);
-    hsrc[mb] = reinterpret_cast<const char*>(hidden + (int64_t)row * K) + unit(wave) * 16;
+  for (int i = 0; i < kHOps; ++i) {
+    hblk[i] = min(wave + i * NW, kHBlocks - 1);
+    hoff[i] = (uint32_t)min(8 * hblk[i] + (lane >> 3), M - 1 - m0) * (uint32_t)K + unit(hblk[i]) * 16;
   }
-  const float* ssrc = hidden_scale + min(m0 + (int)threadIdx.x, M - 1);
+  const uint32_t soff = (uint32_t)min((int)(threadIdx.x & 255), M - 1 - m0) * 4u;
   const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)lds;
-  // DMA j of line c into stage s.
-  auto issue_op = [&](int j, int s, int c) {
+  // DMA j of line c into stage s, of its first `units` units (the others repeat the first).
+  auto issue_op = [&](int j, int s, int c, int units = 8) {
     const uint32_t dst = lds_base + (uint32_t)s * kStage;
-    const bool part = last_units < 8 && c == nlines - 1;
     const int64_t o = (int64_t)c * kLineBytes;
-    if (j < MB) {
-      const int u = unit(wave);
-      line_dma<false>(hsrc[j] + o + (part && u >= last_units ? (u % last_units - u) * 16 : 0), dst + (4 * j + wave) * 1024);
-    } else if (j < MB + 4 * NB) {
-      const int nb = (j - MB) >> 2, q = (j - MB) & 3;
-      const int u = unit(q);
-      line_dma<true>(wsrc[nb][q] + o + (part && u >= last_units ? (u % last_units - u) * 16 : 0),
-                     dst + (kHBlocks + (wave * NB + nb) * 4 + q) * 1024);
-    } else {
-      word_dma(ssrc + (int64_t)c * M, dst + kScaleAt + wave * 256);
+    uint32_t back = 0;
+    if (units < 8 && j < 4 + kHOps) {
+      const int u = unit(j < 4 ? j : hblk[j < 4 ? 0 : j - 4]);
+      back = u >= units ? (uint32_t)u * 16 : 0;
     }
+    if (j < 4)
+      base_dma<true>(wbase + o, woff[j] - back, dst + (kHBlocks + wave * 4 + j) * 1024);
+    else if (j < 4 + kHOps)
+      base_dma<false>(hbase + o, hoff[j - 4] - back, dst + hblk[j - 4] * 1024);
+    else
+      base_dma_word(hidden_scale + (int64_t)c * M + m0, soff, dst + kScaleAt + (wave & 3) * 256);
   };
-  // Units 2 j and 2 j + 1 of the rows of W block nb, of hidden block mb.
+  // Units 2 j and 2 j + 1 of the wave's W rows, of the rows of hidden group mb.
   const int r = lane & 31;
-  auto slot = [&](int s, int j) {
+  auto at = [&](int s, int j) {
     return lds + s * kStage + (r >> 3) * 1024 + (r & 7) * 128 + ((2 * j + (lane >> 5) + (r >> 1)) & 7) * 16;
   };
-  auto read_w = [&](int s, int nb, int j) {
-    return *reinterpret_cast<const u32x4*>(slot(s, j) + (kHBlocks + (wave * NB + nb) * 4) * 1024);
-  };
-  auto read_h = [&](int s, int mb, int j) { return *reinterpret_cast<const u32x4*>(slot(s, j) + 4 * mb * 1024); };
+  auto read = [&](const unsigned char* p, int group) { return *reinterpret_cast<const u32x4*>(p + 4 * group * 1024); };
 
-  f32x16 acc[MB][NB];
+  f32x16 acc[MB][1];
 #pragma unroll
   for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) acc[mb][nb][e] = 0.f;
+    for (int e = 0; e < 16; ++e) acc[mb][0][e] = 0.f;
 
-  // A wave's entries lie in one block of 128: lane j holds its scale of line c0 + j.
-  const float* wsc = w_scale + (int64_t)min(blk0 * 32 / kColBlock, (V - 1) / kColBlock) * nlines;
+  // A wave's entries lie in one block of 128: lane j holds its scale of line 64 n + j.
+  const float* wsc = w_scale + (int64_t)min(blk0 * 32 / kColBlock, (V - 1) / kColBlock) * nscales;
   float sw_all = 0.f;
 
+  // Tiles start on different lines and wrap: rows a multiple of 4 KB apart would
+  // otherwise send every workgroup to the same memory channels at once.
+  int l = nlines > 0 ? (int)((unsigned)tile % (unsigned)nlines) : 0, next = l;
 #pragma unroll
   for (int c = 0; c < S - 1; ++c)
     if (c < nlines) {
 #pragma unroll
-      for (int j = 0; j < kOps; ++j) issue_op(j, c, c);
+      for (int j = 0; j < kOps; ++j) issue_op(j, c, next);
+      next = next + 1 == nlines ? 0 : next + 1;
     }
   int s = 0;
-  for (int c = 0; c < nlines; ++c) {
-    if ((c & 63) == 0) sw_all = wsc[min(c + lane, nlines - 1)];
-    // Line c is in once only the lines after it are in flight; past the barrier
-    // every wave's part is, and line c - 1 has been read by all.
-    if (c + S - 1 <= nlines)
-      wait_vmcnt<(S - 2) * kOps>();
+  // One line: the products of its 128 columns, from zero, times both scales.
+  // FILL: the line that takes the place of the last one's is asked for bit by
+  // bit meanwhile: a CU keeps about 100 lines in flight, and a wave that asks
+  // for more stands still.
+  auto line = [&](auto fill) {
+    constexpr bool kFill = decltype(fill)::value;
+    if (kFill)
+      wait_vmcnt<(S - 2) * kOps>();  // this line is in once only the lines after it are in flight
     else
       wait_vmcnt<0>();
-    lds_barrier();
-    if (c + S - 1 < nlines) {
-      const int sp = s == 0 ? S - 1 : s - 1;
+    lds_barrier();  // every wave's part is, and the last line has been read by all
+    const int sp = s == 0 ? S - 1 : s - 1;
+    const float sw = lane_f32(sw_all, l & 63);
+    const float* sa = reinterpret_cast<const float*>(lds + s * kStage + kScaleAt) + r;
+    constexpr f32x16 kZero = {};
+    const unsigned char* p[4];
 #pragma unroll
-      for (int j = 0; j < kOps; ++j) issue_op(j, sp, c + S - 1);
+    for (int j = 0; j < 4; ++j) p[j] = at(s, j);
+    bf16x8 wf[8];
+    u32x4 x[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = read(p[j], 0);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const u32x4 y = *reinterpret_cast<const u32x4*>(p[j] + (kHBlocks + wave * 4) * 1024);
+      wf[2 * j] = widen8(y[0], y[1], 1.f);
+      wf[2 * j + 1] = widen8(y[2], y[3], 1.f);
     }
-    const float sw = lane_f32(sw_all, c & 63);
-    const float* sa = reinterpret_cast<const float*>(lds + s * kStage + kScaleAt);
-    if (last_units == 8 || c + 1 < nlines) {
-      bf16x8 wf[NB][8];
+    // A group's sum is added, scaled, while the next group is multiplied.
+    f32x16 sum[2];
+    float f[2];
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
+    for (int mb = 0; mb < MB; ++mb) {
+      f[mb & 1] = sa[mb * 32] * sw;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const u32x4 x = read_w(s, nb, j);
-          wf[nb][2 * j] = widen8(x[0], x[1], 1.f);
-          wf[nb][2 * j + 1] = widen8(x[2], x[3], 1.f);
+      for (int j = 0; j < 4; ++j) {
+        const bf16x8 h0 = widen8(x[j][0], x[j][1], 1.f), h1 = widen8(x[j][2], x[j][3], 1.f);
+        if (mb + 1 < MB) x[j] = read(p[j], mb + 1);
+        sum[mb & 1] = mfma32x32x16(wf[2 * j], h0, j == 0 ? kZero : sum[mb & 1]);
+        if (mb > 0) {
+#pragma unroll
+          for (int e = 4 * j; e < 4 * j + 4; ++e)
+            acc[mb - 1][0][e] = fmaf(sum[(mb - 1) & 1][e], f[(mb - 1) & 1], acc[mb - 1][0][e]);
         }
+        sum[mb & 1] = mfma32x32x16(wf[2 * j + 1], h1, sum[mb & 1]);
+        if (kFill) {
+          const int i = 4 * mb + j;
+#pragma unroll
+          for (int o = i * kOps / kSteps; o < (i + 1) * kOps / kSteps; ++o) issue_op(o, sp, next);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      acc[MB - 1][0][e] = fmaf(sum[(MB - 1) & 1][e], f[(MB - 1) & 1], acc[MB - 1][0][e]);
+    if (kFill) next = next + 1 == nlines ? 0 : next + 1;
+    s = s + 1 == S ? 0 : s + 1;
+    l = l + 1 == nlines ? 0 : l + 1;
+  };
+  sw_all = wsc[min((l & ~63) + lane, nscales - 1)];
+  int c = 0;
+  for (; c + S - 1 < nlines; ++c) {
+    if ((l & 63) == 0) sw_all = wsc[min(l + lane, nscales - 1)];
+    line(Flag<true>());
+  }
+  for (; c < nlines; ++c) {
+    if ((l & 63) == 0) sw_all = wsc[min(l + lane, nscales - 1)];
+    line(Flag<false>());
+  }
+  if (nscales > nlines) {  // the columns past the last whole line: 32, 64 or 96
+    const int units = (K - nlines * kColBlock) / 16;
+    lds_barrier();
+#pragma unroll
+    for (int o = 0; o < kOps; ++o) issue_op(o, 0, nlines, units);
+    wait_vmcnt<0>();
+    lds_barrier();
+    const float sw = wsc[nlines];
+    for (int j = 0; j < units / 2; ++j) {
+      const unsigned char* p = at(0, j);
+      const u32x4 y = *reinterpret_cast<const u32x4*>(p + (kHBlocks + wave * 4) * 1024);
+      const bf16x8 w0 = widen8(y[0], y[1], 1.f), w1 = widen8(y[2], y[3], 1.f);
 #pragma unroll
       for (int mb = 0; mb < MB; ++mb) {
-        f32x16 sum[NB];
+        const u32x4 x = read(p, mb);
+        f32x16 sum = {};
+        sum = mfma32x32x16(w0, widen8(x[0], x[1], 1.f), sum);
+        sum = mfma32x32x16(w1, widen8(x[2], x[3], 1.f), sum);
+        const float f = reinterpret_cast<const float*>(lds + kScaleAt)[mb * 32 + r] * sw;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const u32x4 x = read_h(s, mb, j);
-          const bf16x8 h0 = widen8(x[0], x[1], 1.f), h1 = widen8(x[2], x[3], 1.f);
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb) {
-            if (j == 0) {
-#pragma unroll
-              for (int e = 0; e < 16; ++e) sum[nb][e] = 0.f;
-            }
-            sum[nb] = mfma32x32x16(wf[nb][2 * j], h0, sum[nb]);
-          }
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb) sum[nb] = mfma32x32x16(wf[nb][2 * j + 1], h1, sum[nb]);
-        }
-        const float f = sa[mb * 32 + r] * sw;
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) acc[mb][nb][e] = fmaf(sum[nb][e], f, acc[mb][nb][e]);
-      }
-    } else {
-      for (int j = 0; j < last_units / 2; ++j) {
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-          const u32x4 y = read_w(s, nb, j);
-          const bf16x8 w0 = widen8(y[0], y[1], 1.f), w1 = widen8(y[2], y[3], 1.f);
-#pragma unroll
-          for (int mb = 0; mb < MB; ++mb) {
-            const u32x4 x = read_h(s, mb, j);
-            f32x16 sum;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) sum[e] = 0.f;
-            sum = mfma32x32x16(w0, widen8(x[0], x[1], 1.f), sum);
-            sum = mfma32x32x16(w1, widen8(x[2], x[3], 1.f), sum);
-            const float f = sa[mb * 32 + r] * sw;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) acc[mb][nb][e] = fmaf(sum[e], f, acc[mb][nb][e]);
-          }
-        }
+        for (int e = 0; e < 16; ++e) acc[mb][0][e] = fmaf(sum[e], f, acc[mb][0][e]);
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
-    s = s + 1 == S ? 0 : s + 1;
   }
   lds_barrier();
-  tile_epilogue32<MB, NB, NW>(acc, M, V, ntiles, tile, m0, blk0, logits, partials,
-                              reinterpret_cast<float(*)[MB * 32]>(lds));
+  tile_epilogue32<MB, 1, NW>(acc, M, V, ntiles, tile, m0, blk0, logits, partials,
+                             reinterpret_cast<float(*)[MB * 32]>(lds));
 }
 
-template <int MB, int NB>
+template <int MB, int NW>
 hipError_t launch(const Fp8Plan& p, const void* hidden, const float* hidden_scale, const void* w, const float* w_scale,
                   float* logits, float2* partials, hipStream_t stream) {
-  hipLaunchKernelGGL((vocab_fp8_kernel<MB, NB>), dim3((p.ntiles + 7) / 8 * 8 * p.mtiles), dim3(kWaves * kWave), 0,
-                     stream, p.M, p.K, p.V, p.ntiles, p.mtiles, static_cast<const uint8_t*>(hidden), hidden_scale,
+  hipLaunchKernelGGL((vocab_fp8_kernel<MB, NW>), dim3((p.ntiles + 7) / 8 * 8 * p.mtiles), dim3(NW * kWave), 0, stream,
+                     p.M, p.K, p.V, p.ntiles, p.mtiles, static_cast<const uint8_t*>(hidden), hidden_scale,
                      static_cast<const uint8_t*>(w), w_scale, logits, partials);
   return hipGetLastError();
 }
@@ -229,8 +262,8 @@ Fp8Plan fp8_plan(int M, int K, int V) {
   const int blocks = (M + 31) / 32;
   p.mtiles = (blocks + 6) / 7;
   p.mb = (blocks + p.mtiles - 1) / p.mtiles;
-  p.nb = V > 32 * 1024 ? 2 : 1;
-  const int width = 32 * kWaves * p.nb;
+  p.nw = M > 64 || V > 65536 ? 8 : 4;
+  const int width = 32 * p.nw;
   p.ntiles = (V + width - 1) / width;
   return p;
 }
@@ -243,8 +276,8 @@ hipError_t launch_logits_fp8(const Fp8Plan& p, const void* hidden, const float* 
   hipError_t e = hipErrorInvalidValue;
 #define SDV_F(B)                                                                                             \
   case B:                                                                                                    \
-    e = p.nb == 2 ? launch<B, 2>(p, hidden, hidden_scale, w, w_scale, logits, partials, stream)              \
-                  : launch<B, 1>(p, hidden, hidden_scale, w, w_scale, logits, partials, stream);             \
+    e = p.nw == 8 ? launch<B, 8>(p, hidden, hidden_scale, w, w_scale, logits, partials, stream)              \
+                  : launch<B, 4>(p, hidden, hidden_scale, w, w_scale, logits, partials, stream);             \
     break;
   switch (p.mb) {
     SDV_F(1) SDV_F(2) SDV_F(3) SDV_F(4) SDV_F(5) SDV_F(6) SDV_F(7)
