@@ -92,7 +92,7 @@ extern "C" {
 size_t sd_fp8_workspace_bytes(const sd_dims_t* d, int32_t max_kv_len) {
   size_t n = 0;
   if (check_attention(d) == SD_OK && max_kv_len > d->gamma && max_kv_len <= kMaxKvLen) {
-    const int64_t chunks = kv8_max_chunks(d->gamma + 1, d->n_q_heads, d->n_kv_heads, d->head_dim, d->batch, max_kv_len);
+    const int64_t chunks = kv8_max_chunks(d->n_kv_heads, d->batch, max_kv_len);
     const int rows = (d->gamma + 1) * (d->n_q_heads / d->n_kv_heads);
     n = align_up(attn_partial_bytes(chunks, d->n_kv_heads, rows, d->head_dim));
   }
@@ -165,7 +165,7 @@ int sd_verify_attention_kv8(const sd_dims_t* d, const void* q, const sd_kv8_cach
     if (kv_len[b] < G || !length_ok(cache, kv_len[b])) return SD_ERR_INVALID_ARGUMENT;
   const AttnShape s = kv8_shape(G, d->n_q_heads, d->n_kv_heads, d->head_dim, scale, kv_len, d->batch);
   const int64_t chunks = count_chunks(kv_len, d->batch, s.chunk_keys);
-  if (chunks * s.Hkv * s.row_groups > 4 * kMaxGrid) return SD_ERR_UNSUPPORTED;
+  if (chunks * s.Hkv * s.row_groups > kMaxGrid) return SD_ERR_UNSUPPORTED;
   if (workspace_bytes < attention_ws(s, chunks)) return SD_ERR_WORKSPACE;
   const AttnPartials parts = attn_carve(workspace, chunks, s.Hkv, s.rows, s.D);
   const Kv8Pool pool = pool_of(cache);

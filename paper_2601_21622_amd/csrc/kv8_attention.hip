@@ -10,16 +10,19 @@
 // The cache is laid out in the order in which the matrix instructions take
 // their operands (sdverify_fp8.h): a lane's 16 bytes of K are two 32-wide steps
 // of one key, its 16 bytes of V four keys in each of the block's four 16-key
-// score tiles.  So K and V go from HBM into registers in loads of 1 KB in a row
-// each, with no LDS and no transposition: the probabilities that a lane holds
-// after S^T = K Q^T (tile t: keys 16 t + 4 g + r of group g = lane / 16) are the
-// keys that its V bytes hold, which is all that O^T += V^T P^T needs.  Codes
-// widen to bfloat16 with the block's scale in the same instruction, exactly.
-// (The 8-bit matrix instructions would skip that, but they keep too few bits:
-// sums of 128 products come out 1.4e-5 off, and P would have to be 8 bits.)
+// score tiles.  So a fragment is 1 KB in a row everywhere, and nothing is
+// transposed: the probabilities that a lane holds after S^T = K Q^T (tile t:
+// keys 16 t + 4 g + r of group g = lane / 16) are the keys that its V bytes hold,
+// which is all that O^T += V^T P^T needs.  Codes widen to bfloat16 with the
+// block's scale in the same instruction, exactly.  (The 8-bit matrix instructions
+// would skip that, but they keep too few bits: sums of 128 products come out
+// 1.4e-5 off, and P would have to be 8 bits.)
 //
-// The next block's K is loaded when the current one's scores are done, its V
-// when the products with V are: each has half a block's work to arrive.
+// K and V come by LDS DMA into a ring of half blocks (one block's K, or its V) of
+// the wave's own, as many halves ahead as the CU's LDS holds; a half's place is
+// filled again, DMA by DMA, under the products after it is free.  In registers the
+// 128 of a block and its successor would push O out to scratch.
+//
 // Softmax in the log2 domain.  O is never rescaled (a branch that does so made
 // the compiler spill up to 535 registers): the chunk's first block sets each
 // row's reference maximum, and later scores may exceed it by 2^64, far within
@@ -33,13 +36,35 @@ namespace sdv {
 
 namespace {
 
-constexpr int kItems = 4;        // waves, and items, per workgroup
-constexpr int kMaxBlocks = 5;    // 16-row blocks per wave
-constexpr int kMaxTiles = 64;    // blocks per chunk: one lane holds one block's page
+constexpr int kItems = 4;       // workgroups of one wave, an item each, per CU
+constexpr int kMaxBlocks = 5;   // 16-row blocks of a wave
+constexpr int kMaxTiles = 64;   // blocks per chunk: one lane holds one block's page
 constexpr float kGrowLog2 = 64.f;  // growth of a row's maximum that takes the item up anew
+
+// A wave's ring: halves of 64 D bytes, D / 16 DMAs of 1 KB each.  Four fill a CU's
+// 160 KB (D = 128).
+template <int D>
+struct Ring {
+  static constexpr int kHalf = D * kKeyBlock;
+  static constexpr int kOps = D / 16;
+  static constexpr int kSlots = D == 128 ? 5 : 8;
+};
 
 typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
 typedef __attribute__((__vector_size__(2 * sizeof(float)))) float f32x2;
+
+template <bool X>
+struct Kind {
+  static constexpr bool value = X;
+};
+
+// LDS DMA of 1 KB: lane l copies 16 bytes from base + off into LDS bytes lds +
+// 16 l (lds wave-uniform).  From inline assembly, so that the compiler adds no
+// waits of its own; the wait state between the write of M0 and the load is here.
+__device__ __forceinline__ void ring_dma(const void* base, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt"
+               : : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(off), "s"(base) : "m0", "memory");
+}
 
 __device__ __forceinline__ float max_over_groups(float v) {
   const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -104,33 +129,51 @@ struct Wave8 {
   uint32_t nan;        // a NaN code was left out of O
 };
 
-// Scores of one 64-key block less `base`: the accumulators start there, so that
-// the difference that the exponential takes costs no instruction and keeps its
-// bits however large the scores are.  MASKED: some key lies past `first`, the
-// first of the step's positions; what a row does not see is -inf.
-template <int RB, int D, bool MASKED>
-__device__ __forceinline__ void block_scores(const Wave8<RB, D>& w, const u32x4 (&kr)[4][D / 64], float ks, int off,
-                                             const float (&base)[RB], f32x4 (&sc)[RB][4]) {
+// The instructions since the last call as M products with at most V vector
+// instructions among them, one product first, so that the vector ones issue
+// while the matrix core works.
+template <int M, int V>
+__device__ __forceinline__ void interleave() {
 #pragma unroll
-  for (int t = 0; t < 4; ++t) {
+  for (int i = 0; i < M; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x002, (V + M - 1) / M, 0);
+  }
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// Scores of half `hf` of a 64-key block (its score tiles 2 hf and 2 hf + 1) less
+// `base`: the accumulators start there, so that the difference that the
+// exponential takes costs no instruction and keeps its bits however large the
+// scores are.  MASKED: some key lies past `first`, the first of the step's
+// positions; what a row does not see is -inf.
+template <int RB, int D, bool MASKED, typename Refill>
+__device__ __forceinline__ void half_scores(const Wave8<RB, D>& w, const u32x4 (&k)[2][D / 64], int hf, float ks,
+                                            int off, const float (&base)[RB], f32x4 (&sc)[RB][2], Refill refill) {
+  constexpr int kSteps = D / 32;  // 32-wide steps of a score tile
+  auto widen_k = [&](int n) {
+    const u32x4 x = k[n / kSteps][n % kSteps / 2];
+    return widen8(x[2 * (n & 1)], x[2 * (n & 1) + 1], ks);
+  };
+  bf16x8 kf = widen_k(0);
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) sc[rb][t] = f32x4{base[rb], base[rb], base[rb], base[rb]};
+  for (int n = 0; n < 2 * kSteps; ++n) {
+    const int t = n / kSteps;
+    const bf16x8 now = kf;
+    if (n + 1 < 2 * kSteps) kf = widen_k(n + 1);  // under this step's products
 #pragma unroll
-    for (int i = 0; i < D / 64; ++i)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const bf16x8 kf = widen8(kr[t][i][2 * h], kr[t][i][2 * h + 1], ks);
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) sc[rb][t] = mfma16x16x32(kf, w.q[rb][2 * i + h], sc[rb][t]);
-      }
-    __builtin_amdgcn_sched_barrier(0);
+    for (int rb = 0; rb < RB; ++rb)
+      sc[rb][t] = mfma16x16x32(now, w.q[rb][n % kSteps],
+                               n % kSteps == 0 ? f32x4{base[rb], base[rb], base[rb], base[rb]} : sc[rb][t]);
+    if (n % kSteps == kSteps - 1) refill(2 * hf + t);
+    interleave<RB, 4>();
   }
   if (MASKED) {
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-      const uint64_t win = keys_seen(w.sees[rb], off);
+      const uint64_t win = keys_seen(w.sees[rb], off) >> (32 * hf);
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
+      for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const uint32_t see = (uint32_t)(win >> (16 * t + r)) & 1u;
@@ -141,88 +184,116 @@ __device__ __forceinline__ void block_scores(const Wave8<RB, D>& w, const u32x4 
   }
 }
 
-// Each row's largest score of the block.
+// K fragments of half `hf` of the block at kp.
+template <int D>
+__device__ __forceinline__ void read_k(const unsigned char* kp, int hf, u32x4 (&k)[2][D / 64]) {
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) k[t][i] = *reinterpret_cast<const u32x4*>(kp + (i * 4 + 2 * hf + t) * 1024);
+}
+
+// Each row's largest score of the half.
 template <int RB>
-__device__ __forceinline__ void block_max(const f32x4 (&sc)[RB][4], float (&mx)[RB]) {
+__device__ __forceinline__ void half_max(const f32x4 (&sc)[RB][2], float (&mx)[RB]) {
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
     float x = fmaxf(fmaxf(sc[rb][0][0], sc[rb][0][1]), fmaxf(sc[rb][0][2], sc[rb][0][3]));
-#pragma unroll
-    for (int t = 1; t < 4; ++t)
-      x = fmaxf(fmaxf(fmaxf(x, sc[rb][t][0]), sc[rb][t][1]), fmaxf(sc[rb][t][2], sc[rb][t][3]));
+    x = fmaxf(fmaxf(fmaxf(x, sc[rb][1][0]), sc[rb][1][1]), fmaxf(sc[rb][1][2], sc[rb][1][3]));
     mx[rb] = max_over_groups(x);
   }
 }
 
-// Folds one block into O and the sums; false, and nothing folded, when some
-// row's maximum has outgrown its reference.  load_k and load_v fetch the next
-// block once kr and vr are free.
-template <int RB, int D, bool MASKED, typename LoadK, typename LoadV>
-__device__ __forceinline__ bool fold_block(Wave8<RB, D>& w, u32x4 (&kr)[4][D / 64], u32x4 (&vr)[D / 16], float ks,
-                                           float vs, float scale_log2, int key0, int first, int end, LoadK load_k,
-                                           LoadV load_v) {
+// Folds one block, half after half, into O and the sums; false when some row's
+// maximum has outgrown its reference (O is then not whole).  refill_v and
+// refill_k take quarter `n` of the DMAs into the places of the last block's V and
+// of this one's K; wait_v waits for this block's V.
+template <int RB, int D, bool MASKED, typename WaitV, typename RefillV, typename RefillK>
+__device__ __forceinline__ bool fold_block(Wave8<RB, D>& w, const unsigned char* kp, const unsigned char* vp, float ks,
+                                           float vs, float scale_log2, int key0, int first, int end, WaitV wait_v,
+                                           RefillV refill_v, RefillK refill_k) {
   const int lg = (threadIdx.x & 63) >> 4;
-  f32x4 sc[RB][4];
-  float base[RB], mx[RB];
-#pragma unroll
-  for (int rb = 0; rb < RB; ++rb) base[rb] = w.m[rb] > kNegBig ? -w.m[rb] : 0.f;
-  block_scores<RB, D, MASKED>(w, kr, ks, key0 + 4 * lg - first, base, sc);
-  load_k();
-  block_max<RB>(sc, mx);
-  bool grow = false;
-#pragma unroll
-  for (int rb = 0; rb < RB; ++rb) grow |= mx[rb] * scale_log2 > (w.m[rb] > kNegBig ? kGrowLog2 : kNegBig);
-  if (__builtin_expect(__ballot(grow) != 0, 0)) return false;
-  // P in bfloat16, as the products take it; the sum adds the rounded values,
-  // so that the weights that O accumulates sum to one.
-  bf16x8 pf[RB][2];
   const bf16x2 ones = {(__bf16)1.f, (__bf16)1.f};
+  // V fragments in flight from LDS: a fragment's RB products cover its successors' latency.
+  constexpr int kAhead = RB == 1 ? 8 : RB == 2 ? 4 : 2;
+  u32x4 k[2][D / 64];
+  read_k<D>(kp, 0, k);
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    float acc = w.l[rb];
+  for (int hf = 0; hf < 2; ++hf) {
+    f32x4 sc[RB][2];
+    float base[RB], mx[RB];
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int r = 0; r < 4; r += 2) {
-        const f32x2 x = {__builtin_amdgcn_exp2f(sc[rb][t][r] * scale_log2),
-                         __builtin_amdgcn_exp2f(sc[rb][t][r + 1] * scale_log2)};
-        const bf16x2 pb = __builtin_convertvector(x, bf16x2);
-        pf[rb][t / 2][(t & 1) * 4 + r] = pb[0];
-        pf[rb][t / 2][(t & 1) * 4 + r + 1] = pb[1];
-        acc = __builtin_amdgcn_fdot2_f32_bf16(pb, ones, acc, false);
-      }
-    w.l[rb] = acc;
-  }
-  if (MASKED) {
-    // What lies past the last key is not read as numbers, and NaN codes are
-    // left to spread_nan: 0 * NaN would reach the rows that do not see them.
-#pragma unroll
-    for (int db = 0; db < D / 16; ++db)
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        vr[db][t] &= bytes_before(key0 + 16 * t + 4 * lg, end);
-        const uint32_t hit = nan_bytes(vr[db][t]);
-        w.nan |= hit;
-        vr[db][t] &= ~(hit * 0xffu);
-      }
-  }
-#pragma unroll
-  for (int db = 0; db < D / 16; ++db)
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const bf16x8 vf = widen8(vr[db][2 * h], vr[db][2 * h + 1], vs);
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) w.o[rb][db] = mfma16x16x32(vf, pf[rb][h], w.o[rb][db]);
-      if (h == 1 && (db & 1)) __builtin_amdgcn_sched_barrier(0);
+    for (int rb = 0; rb < RB; ++rb) base[rb] = w.m[rb] > kNegBig ? -w.m[rb] : 0.f;
+    half_scores<RB, D, MASKED>(w, k, hf, ks, key0 + 4 * lg - first, base, sc, refill_v);
+    if (hf == 0) {
+      read_k<D>(kp, 1, k);
+      wait_v();
     }
-  load_v();
+    u32x2 v_in[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead && i < D / 16; ++i) v_in[i] = *reinterpret_cast<const u32x2*>(vp + i * 1024 + 8 * hf);
+    half_max<RB>(sc, mx);
+    bool grow = false;
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) grow |= mx[rb] * scale_log2 > (w.m[rb] > kNegBig ? kGrowLog2 : kNegBig);
+    if (__builtin_expect(__ballot(grow) != 0, 0)) return false;
+    // P in bfloat16, as the products take it; the sum adds the rounded values,
+    // so that the weights that O accumulates sum to one.
+    bf16x8 pf[RB];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      float acc = w.l[rb];
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; r += 2) {
+          const f32x2 x = {__builtin_amdgcn_exp2f(sc[rb][t][r] * scale_log2),
+                           __builtin_amdgcn_exp2f(sc[rb][t][r + 1] * scale_log2)};
+          const bf16x2 pb = __builtin_convertvector(x, bf16x2);
+          pf[rb][t * 4 + r] = pb[0];
+          pf[rb][t * 4 + r + 1] = pb[1];
+          acc = __builtin_amdgcn_fdot2_f32_bf16(pb, ones, acc, false);
+        }
+      w.l[rb] = acc;
+    }
+    // Fragment db of V, cleared where it must not be read as numbers.
+    auto widen_v = [&](int db) {
+      u32x2 v = v_in[db % kAhead];
+      if (db + kAhead < D / 16) v_in[db % kAhead] = *reinterpret_cast<const u32x2*>(vp + (db + kAhead) * 1024 + 8 * hf);
+      if (MASKED) {
+        // What lies past the last key is no number, and NaN codes are left to
+        // spread_nan: 0 * NaN would reach the rows that do not see them.
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          v[t] &= bytes_before(key0 + 32 * hf + 16 * t + 4 * lg, end);
+          const uint32_t hit = nan_bytes(v[t]);
+          w.nan |= hit;
+          v[t] &= ~(hit * 0xffu);
+        }
+      }
+      return widen8(v[0], v[1], vs);
+    };
+    bf16x8 vf = widen_v(0);
+#pragma unroll
+    for (int db = 0; db < D / 16; ++db) {
+      const bf16x8 now = vf;
+      if (db + 1 < D / 16) vf = widen_v(db + 1);  // under this fragment's products
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) w.o[rb][db] = mfma16x16x32(now, pf[rb], w.o[rb][db]);
+      if (hf == 1 && db % (D / 64) == D / 64 - 1) refill_k(db / (D / 64));
+      if (MASKED)
+        __builtin_amdgcn_sched_barrier(0);
+      else
+        interleave<RB, 4>();
+    }
+  }
   return true;
 }
 
 // Makes the outputs NaN that a NaN code of this block reaches: those of the rows
 // that see its key, in its column.
 template <int RB, int D>
-__device__ __forceinline__ void spread_nan(Wave8<RB, D>& w, u32x4 (&vr)[D / 16], int key0, int first, int end) {
+__device__ __forceinline__ void spread_nan(Wave8<RB, D>& w, const unsigned char* vp, int key0, int first, int end) {
   const int lg = (threadIdx.x & 63) >> 4;
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
@@ -232,9 +303,10 @@ __device__ __forceinline__ void spread_nan(Wave8<RB, D>& w, u32x4 (&vr)[D / 16],
     for (int j = 0; j < 16; ++j) sf[j >> 3][j & 7] = (__bf16)(float)((uint32_t)(win >> (16 * (j >> 2) + (j & 3))) & 1u);
 #pragma unroll
     for (int db = 0; db < D / 16; ++db) {
+      const u32x4 v = *reinterpret_cast<const u32x4*>(vp + db * 1024);
       u32x4 ind;  // 1 (code 0x38) where V is NaN
 #pragma unroll
-      for (int t = 0; t < 4; ++t) ind[t] = nan_bytes(vr[db][t] & bytes_before(key0 + 16 * t + 4 * lg, end)) * 0x38u;
+      for (int t = 0; t < 4; ++t) ind[t] = nan_bytes(v[t] & bytes_before(key0 + 16 * t + 4 * lg, end)) * 0x38u;
       f32x4 n = {0.f, 0.f, 0.f, 0.f};
       n = mfma16x16x32(widen8(ind[0], ind[1], 1.f), sf[0], n);
       n = mfma16x16x32(widen8(ind[2], ind[3], 1.f), sf[1], n);
@@ -246,25 +318,30 @@ __device__ __forceinline__ void spread_nan(Wave8<RB, D>& w, u32x4 (&vr)[D / 16],
 }
 
 template <int RB, int D>
-__global__ __launch_bounds__(kItems * kWave, (RB <= 2 ? 2 : 1))
-void kv8_attn_kernel(AttnShape s, AttnBatch bt, Kv8Pool pool, int nitems, const uint16_t* __restrict__ q,
+__global__ __launch_bounds__(kWave, 1)
+void kv8_attn_kernel(AttnShape s, AttnBatch bt, Kv8Pool pool, int nchunks, const uint16_t* __restrict__ q,
                      AttnPartials parts) {
+  using R = Ring<D>;
+  __shared__ __align__(1024) unsigned char ring[R::kSlots * R::kHalf];
   const int lane = threadIdx.x & 63;
   const int lr = lane & 15, lg = lane >> 4;
-  const int item = __builtin_amdgcn_readfirstlane(blockIdx.x * kItems + (threadIdx.x >> 6));
-  if (item >= nitems) return;
-  // Row groups of one (chunk, KV head) are neighbours: their second reads of a block hit cache.
-  const int rg = item % s.row_groups;
-  const int head = item / s.row_groups % s.Hkv;
-  const int c = item / s.row_groups / s.Hkv;
+  // Row groups of one (chunk, KV head) are 8 workgroups apart, on one XCD: the
+  // second read of a block hits its L2.
+  const int per = 8 * s.row_groups;
+  const int item = blockIdx.x / per * 8 + (blockIdx.x & 7);
+  const int rg = blockIdx.x % per >> 3;
+  if (item >= nchunks * s.Hkv) return;
+  const int head = item % s.Hkv;
+  const int c = item / s.Hkv;
   int lo = 0, hi = bt.nreq - 1;  // the largest request with chunk_prefix <= c
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
     if (bt.chunk_prefix[mid] <= c) lo = mid; else hi = mid - 1;
   }
+  lo = __builtin_amdgcn_readfirstlane(lo);
   const int req = bt.req0 + lo;
-  const int end = bt.kv_len[lo], first = end - s.G;
-  const int key_begin = (c - bt.chunk_prefix[lo]) * s.chunk_keys;
+  const int end = __builtin_amdgcn_readfirstlane(bt.kv_len[lo]), first = end - s.G;
+  const int key_begin = (c - __builtin_amdgcn_readfirstlane(bt.chunk_prefix[lo])) * s.chunk_keys;
   const int key_end = min(key_begin + s.chunk_keys, end);
   const int ntiles = (key_end - key_begin + kKeyBlock - 1) / kKeyBlock;
   const int blk0 = key_begin / kKeyBlock;
@@ -278,25 +355,36 @@ void kv8_attn_kernel(AttnShape s, AttnBatch bt, Kv8Pool pool, int nitems, const 
   const uint32_t at_lo = (uint32_t)at, at_hi = (uint32_t)(at >> 32);
   const int ks_all = pool.k_scale[at], vs_all = pool.v_scale[at];
 
-  u32x4 kr[4][D / 64], vr[D / 16];
-  auto tile_at = [&](int t) {
-    return (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)at_hi, t) << 32) |
-                     (uint32_t)__builtin_amdgcn_readlane((int)at_lo, t)) * (D * kKeyBlock);
-  };
-  auto load_k = [&](int t) {
-    const uint8_t* p = pool.k + tile_at(min(t, ntiles - 1));
+  const uint32_t ring_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)ring;
+  const uint32_t off = lane * 16;
+  // DMAs i .. n - 1 of half `half` (block half / 2: K, then V) into place `slot`.
+  auto fetch = [&](int half, int slot, int i, int n) {
+    const int t = half >> 1;
+    const int64_t blk_at = (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)at_hi, t) << 32) |
+                                     (uint32_t)__builtin_amdgcn_readlane((int)at_lo, t));
+    const uint8_t* src = ((half & 1) ? pool.v : pool.k) + blk_at * R::kHalf;
+    const uint32_t dst = ring_at + slot * R::kHalf;
 #pragma unroll
-    for (int i = 0; i < D / 64; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) kr[j][i] = load_u32x4_stream(p + (i * 4 + j) * 1024 + lane * 16);
+    for (int j = i; j < n; ++j) ring_dma(src + j * 1024, off, dst + j * 1024);
   };
-  auto load_v = [&](int t) {
-    const uint8_t* p = pool.v + tile_at(min(t, ntiles - 1));
-#pragma unroll
-    for (int i = 0; i < D / 16; ++i) vr[i] = load_u32x4_stream(p + i * 1024 + lane * 16);
+  const int halves = __builtin_amdgcn_readfirstlane(2 * ntiles);
+  // Half n is in: of those after it, as many as are on their way may still be.
+  auto wait_half = [&](int n) {
+    static_assert((R::kSlots - 2) * R::kOps < 64, "vmcnt holds 6 bits");
+    const int after = halves - 1 - n;
+    if (after >= R::kSlots - 2) wait_vmcnt<(R::kSlots - 2) * R::kOps>();
+    else if (after >= 3) wait_vmcnt<3 * R::kOps>();
+    else if (after == 2) wait_vmcnt<2 * R::kOps>();
+    else if (after == 1) wait_vmcnt<R::kOps>();
+    else wait_vmcnt<0>();
+    asm volatile("" ::: "memory");
   };
-  load_k(0);
-  load_v(0);
+  auto fill = [&] {
+#pragma unroll
+    for (int n = 0; n < R::kSlots; ++n)
+      if (n < halves) fetch(n, n, 0, R::kOps);
+  };
+  fill();
 
   Wave8<RB, D> w;
   const uint64_t masks = position_mask(bt.parent != nullptr ? bt.parent + (int64_t)req * (s.G - 1) : nullptr, s.G);
@@ -320,46 +408,76 @@ void kv8_attn_kernel(AttnShape s, AttnBatch bt, Kv8Pool pool, int nitems, const 
   int from = 0, to = 1;  // blocks whose maxima are taken before the next fold
   for (;;) {
     for (int t = from; t < to; ++t) {
-      if (t > 0) load_k(t);
-      f32x4 sc[RB][4];
-      float zero[RB], mx[RB];
+      if (from == 0) {
+        wait_half(0);
+      } else {
+        fetch(2 * t, 0, 0, R::kOps);
+        wait_vmcnt<0>();
+        asm volatile("" ::: "memory");
+      }
+      float zero[RB];
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) zero[rb] = 0.f;
-      block_scores<RB, D, true>(w, kr, pow2(ks_all, t), key_begin + t * kKeyBlock + 4 * lg - first, zero, sc);
-      block_max<RB>(sc, mx);
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb) w.m[rb] = fmaxf(w.m[rb], mx[rb]);
+      for (int hf = 0; hf < 2; ++hf) {
+        u32x4 k[2][D / 64];
+        f32x4 sc[RB][2];
+        float mx[RB];
+        read_k<D>(ring + off, hf, k);
+        half_scores<RB, D, true>(w, k, hf, pow2(ks_all, t), key_begin + t * kKeyBlock + 4 * lg - first, zero, sc,
+                                 [](int) {});
+        half_max<RB>(sc, mx);
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) w.m[rb] = fmaxf(w.m[rb], mx[rb]);
+      }
+      lds_wait();  // read before the next DMA overwrites it
     }
-    if (from > 0) {
-      load_k(0);
-      load_v(0);
-    }
+    if (from > 0) fill();
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
       w.l[rb] = 0.f;
 #pragma unroll
       for (int db = 0; db < D / 16; ++db) w.o[rb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
+    w.nan = 0;
     // Two loops: in one, the compiler widens the codes before it branches to
     // either kind of block, and spills what that takes.
-    w.nan = 0;
-    int t = 0;
+    int t = 0, ks = 0;  // ks: place of K of block t
     bool done = true;
-    for (; t < whole && done; ++t)
-      done = fold_block<RB, D, false>(w, kr, vr, pow2(ks_all, t), pow2(vs_all, t), s.scale_log2, 0, 0, 0,
-                                      [&] { load_k(t + 1); }, [&] { load_v(t + 1); });
-    for (; t < ntiles && done; ++t)
-      done = fold_block<RB, D, true>(w, kr, vr, pow2(ks_all, t), pow2(vs_all, t), s.scale_log2,
-                                     key_begin + t * kKeyBlock, first, end, [&] { load_k(t + 1); }, [&] { load_v(t + 1); });
+    auto step = [&](int block, auto masked) {
+      constexpr bool MASKED = decltype(masked)::value;
+      const int t = __builtin_amdgcn_readfirstlane(block);  // scalar branches
+      const int vs = ks + 1 == R::kSlots ? 0 : ks + 1;    // place of V of block t
+      const int last = ks == 0 ? R::kSlots - 1 : ks - 1;  // of V of block t - 1, free now
+      const int nv = 2 * t - 1 + R::kSlots, nk = nv + 1;  // the halves that take free places
+      wait_half(2 * t);
+      done = fold_block<RB, D, MASKED>(
+          w, ring + ks * R::kHalf + off, ring + vs * R::kHalf + off, pow2(ks_all, t), pow2(vs_all, t), s.scale_log2,
+          key_begin + t * kKeyBlock, first, end, [&] { wait_half(2 * t + 1); },
+          [&](int n) {
+            if (t > 0 && nv < halves) fetch(nv, last, n * R::kOps / 4, (n + 1) * R::kOps / 4);
+          },
+          [&](int n) {
+            if (nk < halves) fetch(nk, ks, n * R::kOps / 4, (n + 1) * R::kOps / 4);
+          });
+      ks = vs + 1 == R::kSlots ? 0 : vs + 1;
+    };
+    for (; t < whole && done; ++t) step(t, Kind<false>());
+    for (; t < ntiles && done; ++t) step(t, Kind<true>());
     if (done) break;
     from = t - 1;
     to = ntiles;
+    wait_vmcnt<0>();
+    lds_wait();
   }
 
   if (__builtin_expect(__ballot(w.nan != 0) != 0, 0)) {
-    for (int t = whole; t < ntiles; ++t) {
-      load_v(t);
-      spread_nan<RB, D>(w, vr, key_begin + t * kKeyBlock, first, end);
+    for (int n = whole; n < ntiles; ++n) {
+      lds_wait();
+      fetch(2 * n + 1, 0, 0, R::kOps);
+      wait_vmcnt<0>();
+      asm volatile("" ::: "memory");
+      spread_nan<RB, D>(w, ring + off, key_begin + n * kKeyBlock, first, end);
     }
   }
 
@@ -439,19 +557,13 @@ int64_t cu_count() {
   return n;
 }
 
-int row_groups(int rows) {
-  const int blocks = (rows + 15) / 16;
-  return (blocks + kMaxBlocks - 1) / kMaxBlocks;
-}
-int blocks_per_wave(int rows) {
+// One wave holds up to five 16-row blocks (at head dimension 128 O takes 32
+// registers of each, Q 16); more rows are split over row groups, a wave each.
+int row_groups(int rows) { return (rows + 16 * kMaxBlocks - 1) / (16 * kMaxBlocks); }
+int blocks_of(int rows) {
   const int g = row_groups(rows);
   return ((rows + 15) / 16 + g - 1) / g;
 }
-
-// Chunk lengths, in 64-key blocks.
-constexpr int kChunks[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 64};
-constexpr int kNumChunks = sizeof(kChunks) / sizeof(kChunks[0]);
-static_assert(kChunks[kNumChunks - 1] == kMaxTiles, "the longest chunk fills a wave's lanes");
 
 }  // namespace
 
@@ -465,51 +577,59 @@ AttnShape kv8_shape(int G, int Hq, int Hkv, int D, float scale, const int32_t* k
   s.rows = G * s.group;
   s.row_groups = row_groups(s.rows);
   s.scale_log2 = scale * kLog2e;
-  // Rounds of items over the wave slots, times an item's length with its
-  // start-up (rows, pages, first block, partial; in keys).
-  const int64_t per_chunk = (int64_t)Hkv * s.row_groups;
-  const int64_t slots = cu_count() * (blocks_per_wave(s.rows) <= 2 ? 8 : 4);
+  // For one to four rounds of items over the CUs' places the shortest chunk that
+  // fits them; of these the one with the least rounds x (chunk + an item's start:
+  // rows, pages, first block, partial, in keys).  More items than four rounds
+  // only with the longest chunk: the workspace holds no more partials.
+  const int64_t slots = cu_count() * kItems;
   const int64_t start = 192 + 2 * s.rows;
+  auto items = [&](int tiles) {
+    const int keys = tiles * kKeyBlock;
+    int64_t n = 0;
+    for (int b = 0; b < B; ++b) n += (kv_len[b] + keys - 1) / keys;
+    return n * Hkv * s.row_groups;
+  };
   int64_t best = INT64_MAX;
+  int most = kMaxTiles;
   s.chunk_keys = kMaxTiles * kKeyBlock;
-  for (int i = kNumChunks - 1; i >= 0; --i) {
-    const int keys = kChunks[i] * kKeyBlock;
-    int64_t chunks = 0;
-    for (int b = 0; b < B; ++b) chunks += (kv_len[b] + keys - 1) / keys;
-    const int64_t items = chunks * per_chunk;
-    if (items > 4 * slots && i < kNumChunks - 1) break;  // shorter chunks: more partials than the workspace holds
-    const int64_t cost = (items + slots - 1) / slots * (keys + start);
+  for (int r = 1; r <= 4; ++r) {
+    if (items(most) > r * slots) continue;
+    int lo = 1, hi = most;  // the shortest chunk lies in [lo, hi]
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      if (items(mid) <= r * slots) hi = mid; else lo = mid + 1;
+    }
+    const int64_t cost = r * (int64_t(lo) * kKeyBlock + start);
     if (cost < best) {
       best = cost;
-      s.chunk_keys = keys;
+      s.chunk_keys = lo * kKeyBlock;
     }
+    most = lo;
+    if (lo == 1) break;
   }
   return s;
 }
 
-int64_t kv8_max_chunks(int G, int Hq, int Hkv, int D, int B, int64_t max_kv_len) {
-  (void)D;
-  const int rows = G * (Hq / Hkv);
-  const int64_t slots = cu_count() * (blocks_per_wave(rows) <= 2 ? 8 : 4);
-  const int64_t most = 4 * slots / ((int64_t)Hkv * row_groups(rows));
+int64_t kv8_max_chunks(int Hkv, int B, int64_t max_kv_len) {
+  const int64_t slots = cu_count() * kItems;
+  const int64_t most = 4 * slots / Hkv;
   const int64_t at_longest = B * ((max_kv_len + kMaxTiles * kKeyBlock - 1) / (kMaxTiles * kKeyBlock));
   return most > at_longest ? most : at_longest;
 }
 
 hipError_t launch_kv8_attention(const AttnShape& s, const AttnBatch& batch, const Kv8Pool& pool, int nchunks,
                                 const void* q, AttnPartials parts, void* out, hipStream_t stream) {
-  const int nitems = nchunks * s.Hkv * s.row_groups;
-  const dim3 grid((nitems + kItems - 1) / kItems), block(kItems * kWave);
-#define SDV_KV8(RB)                                                                                          \
-  case RB:                                                                                                   \
-    if (s.D == 128)                                                                                          \
-      hipLaunchKernelGGL((kv8_attn_kernel<RB, 128>), grid, block, 0, stream, s, batch, pool, nitems,          \
-                         static_cast<const uint16_t*>(q), parts);                                            \
-    else                                                                                                     \
-      hipLaunchKernelGGL((kv8_attn_kernel<RB, 64>), grid, block, 0, stream, s, batch, pool, nitems,           \
-                         static_cast<const uint16_t*>(q), parts);                                            \
+  const dim3 grid((nchunks * s.Hkv + 7) / 8 * 8 * s.row_groups), block(kWave);
+#define SDV_KV8(RB)                                                                                               \
+  case RB:                                                                                                        \
+    if (s.D == 128)                                                                                               \
+      hipLaunchKernelGGL((kv8_attn_kernel<RB, 128>), grid, block, 0, stream, s, batch, pool, nchunks,              \
+                         static_cast<const uint16_t*>(q), parts);                                                 \
+    else                                                                                                          \
+      hipLaunchKernelGGL((kv8_attn_kernel<RB, 64>), grid, block, 0, stream, s, batch, pool, nchunks,               \
+                         static_cast<const uint16_t*>(q), parts);                                                 \
     break;
-  switch (blocks_per_wave(s.rows)) {
+  switch (blocks_of(s.rows)) {
     SDV_KV8(1) SDV_KV8(2) SDV_KV8(3) SDV_KV8(4) SDV_KV8(5)
     default: return hipErrorInvalidValue;
   }
