@@ -7,7 +7,6 @@ sizes, and one device for all.  A call runs on that device (and, without a
 
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import os
 import re
@@ -17,7 +16,7 @@ import numpy as np
 import torch
 
 from . import _binding as _b
-from ._binding import SD_DTYPE_BF16, SD_DTYPE_F32, Dims, _check, _host
+from ._binding import SD_DTYPE_BF16, SD_DTYPE_F32, Dims, _check
 
 SD_KV8_BLOCK = 64
 SD_FP8_BLOCK = 128
@@ -62,9 +61,12 @@ class KV8Cache(ctypes.Structure):
         c._rows = int(block_table.shape[0])
         c._dim = k.numel() // max(1, int(k.shape[0]) * c._heads * page_size)
         c._device = _device(c._tensors)
+        c._ref = ctypes.byref(c)
         return c
 
-    def _fits(self, dims: Dims) -> None:
+    def _fits(self, dims: Dims, dev: int) -> None:
+        if dev != self._device:
+            raise ValueError("device arguments must be on one device")
         if dims.n_kv_heads != self._heads or dims.head_dim != self._dim or dims.batch > self._rows:
             raise ValueError("the cache's heads, head dimension or table rows are not those of dims")
 
@@ -103,9 +105,9 @@ def exported_fp8_symbols() -> list:
 
 # ---- marshalling helpers ------------------------------------------------------
 
-def _device(tensors) -> torch.device:
-    """The one device of the tensors (None among them is left out)."""
-    dev = None
+def _device(tensors) -> int:
+    """The index of the one device of the tensors (None among them is left out)."""
+    dev = -1
     for t in tensors:
         if t is None:
             continue
@@ -113,9 +115,10 @@ def _device(tensors) -> torch.device:
             raise TypeError(f"expected a torch device tensor, got {type(t).__name__}")
         if not t.is_cuda:
             raise ValueError("device arguments must be GPU tensors")
-        if dev is None:
-            dev = t.device
-        elif t.device != dev:
+        d = t.get_device()
+        if dev < 0:
+            dev = d
+        elif d != dev:
             raise ValueError("device arguments must be on one device")
     return dev
 
@@ -126,26 +129,32 @@ def _typed(t, dtype, what: str, elements: int) -> int:
         raise ValueError(f"{what}: expected {dtype}, got {t.dtype}")
     if t.numel() < elements:
         raise ValueError(f"{what}: {t.numel()} elements, {elements} needed")
-    return _b._ptr(t)
+    if not t.is_contiguous():
+        raise ValueError("device arguments must be contiguous")
+    return t.data_ptr()
 
 
 def _lengths(a, dtype, batch: int, what: str):
-    arr, p = _host(a, dtype)
+    arr = np.ascontiguousarray(a, dtype=dtype)
     if arr.size != batch:
         raise ValueError(f"{what}: {arr.size} entries for {batch} requests")
-    return arr, p
+    return arr, arr.__array_interface__["data"][0]
 
 
-def _run(fn, where: str, dev: torch.device, stream, *args) -> None:
-    if isinstance(stream, torch.cuda.Stream):
-        if stream.device != dev:
+def _run(fn, where: str, dev: int, stream, *args) -> None:
+    if stream is None:
+        handle = torch._C._cuda_getCurrentRawStream(dev)
+    elif isinstance(stream, torch.cuda.Stream):
+        if stream.device.index != dev:
             raise ValueError("the stream belongs to another device than the tensors")
         handle = stream.cuda_stream
     else:
-        handle = torch.cuda.current_stream(dev).cuda_stream if stream is None else int(stream)
-    here = dev.index == torch.cuda.current_device()
-    with contextlib.nullcontext() if here else torch.cuda.device(dev):
+        handle = int(stream)
+    if dev == torch._C._cuda_getDevice():
         st = fn(*args, handle)
+    else:
+        with torch.cuda.device(dev):
+            st = fn(*args, handle)
     _check(st, where)
 
 
@@ -169,31 +178,31 @@ def _new_rows(t, dims: Dims, what: str):
 
 def sd_kv8_append(dims: Dims, cache: KV8Cache, k_new, v_new, new_off: Sequence[int], new_len: Sequence[int],
                   kv_len: Sequence[int], stream=None) -> None:
-    dev = _device((*cache._tensors, k_new, v_new))
-    cache._fits(dims)
+    dev = _device((k_new, v_new))
+    cache._fits(dims, dev)
     off, off_p = _lengths(new_off, np.int64, dims.batch, "new_off")
     new, new_p = _lengths(new_len, np.int32, dims.batch, "new_len")
     ln, len_p = _lengths(kv_len, np.int32, dims.batch, "kv_len")
     k, k_stride = _new_rows(k_new, dims, "k_new")
     v, v_stride = _new_rows(v_new, dims, "v_new")
-    if int(np.where(new > 0, off + new, 0).max()) > min(k_new.shape[0], v_new.shape[0]):
+    if int(((off + new) * (new > 0)).max()) > min(k_new.shape[0], v_new.shape[0]):
         raise ValueError("new_off + new_len passes the last new row")
     if k == 0 or v == 0:  # no rows at all: nothing to append
         if k_new.numel() == 0 and v_new.numel() == 0 and not (new > 0).any():
             return
-    _run(_library().sd_kv8_append, "sd_kv8_append", dev, stream, ctypes.byref(dims), ctypes.byref(cache), k, k_stride,
+    _run(_library().sd_kv8_append, "sd_kv8_append", dev, stream, ctypes.byref(dims), cache._ref, k, k_stride,
          v, v_stride, off_p, new_p, len_p)
 
 
 def sd_verify_attention_kv8(dims: Dims, q, cache: KV8Cache, kv_len: Sequence[int], parent, scale: float, out, workspace,
                             stream=None) -> None:
-    dev = _device((q, *cache._tensors, parent, out, workspace))
-    cache._fits(dims)
+    dev = _device((q, parent, out, workspace))
+    cache._fits(dims, dev)
     n = dims.batch * (dims.gamma + 1) * dims.n_q_heads * dims.head_dim
     ln, len_p = _lengths(kv_len, np.int32, dims.batch, "kv_len")
     p = None if parent is None else _typed(parent, torch.int32, "parent", dims.batch * dims.gamma)
     _run(_library().sd_verify_attention_kv8, "sd_verify_attention_kv8", dev, stream, ctypes.byref(dims),
-         _typed(q, torch.bfloat16, "q", n), ctypes.byref(cache), len_p, p, float(scale),
+         _typed(q, torch.bfloat16, "q", n), cache._ref, len_p, p, float(scale),
          _typed(out, torch.bfloat16, "out", n), _b._ptr(workspace), _b._nbytes(workspace))
 
 

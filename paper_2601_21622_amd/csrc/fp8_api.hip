@@ -92,8 +92,8 @@ extern "C" {
 size_t sd_fp8_workspace_bytes(const sd_dims_t* d, int32_t max_kv_len) {
   size_t n = 0;
   if (check_attention(d) == SD_OK && max_kv_len > d->gamma && max_kv_len <= kMaxKvLen) {
-    const int64_t chunks = kv8_max_chunks(d->n_kv_heads, d->batch, max_kv_len);
     const int rows = (d->gamma + 1) * (d->n_q_heads / d->n_kv_heads);
+    const int64_t chunks = kv8_max_chunks(rows, d->n_kv_heads, d->head_dim, d->batch, max_kv_len);
     n = align_up(attn_partial_bytes(chunks, d->n_kv_heads, rows, d->head_dim));
   }
   if (check_projection(d) == SD_OK)
@@ -122,13 +122,13 @@ int sd_kv8_append(const sd_dims_t* d, const sd_kv8_cache_t* cache, const void* k
   for (int b = 0; b < d->batch; ++b) {
     if (new_len[b] > 0) {
       const int64_t blocks = (int64_t(kv_len[b]) + kKeyBlock - 1) / kKeyBlock - (kv_len[b] - new_len[b]) / kKeyBlock;
-      if (blocks > kMaxGrid) return SD_ERR_UNSUPPORTED;
+      if (blocks * d->n_kv_heads * 2 > kMaxGrid) return SD_ERR_UNSUPPORTED;
     }
   }
   for (int b = 0; b < d->batch; ++b) {
     if (new_len[b] > 0) {
       const int blocks = (kv_len[b] + kKeyBlock - 1) / kKeyBlock - (kv_len[b] - new_len[b]) / kKeyBlock;
-      if (a.nreq == kMaxReqPerLaunch || a.blk_prefix[a.nreq] + int64_t(blocks) > kMaxGrid) {
+      if (a.nreq == kMaxReqPerLaunch || (a.blk_prefix[a.nreq] + int64_t(blocks)) * d->n_kv_heads * 2 > kMaxGrid) {
         if (launch_kv8_append(a, pool, d->n_kv_heads, d->head_dim, d->dtype == SD_DTYPE_F32, k_new, k_stride, v_new,
                               v_stride, static_cast<hipStream_t>(stream)) != hipSuccess)
           return SD_ERR_HIP;

@@ -24,8 +24,8 @@
 // 128 of a block and its successor would push O out to scratch.
 //
 // Softmax in the log2 domain.  O is never rescaled (a branch that does so made
-// the compiler spill up to 535 registers): the chunk's first block sets each
-// row's reference maximum, and later scores may exceed it by 2^64, far within
+// the compiler spill up to 535 registers): a row's first scores in the chunk set
+// its reference maximum, and later ones may exceed it by 2^64, far within
 // float32 and bfloat16.  A row that outgrows that makes the wave take the maxima
 // of all blocks from there on and start its item again, once.
 #include <atomic>
@@ -36,18 +36,17 @@ namespace sdv {
 
 namespace {
 
-constexpr int kItems = 4;       // workgroups of one wave, an item each, per CU
 constexpr int kMaxBlocks = 5;   // 16-row blocks of a wave
 constexpr int kMaxTiles = 64;   // blocks per chunk: one lane holds one block's page
 constexpr float kGrowLog2 = 64.f;  // growth of a row's maximum that takes the item up anew
 
-// A wave's ring: halves of 64 D bytes, D / 16 DMAs of 1 KB each.  Four fill a CU's
-// 160 KB (D = 128).
+// A wave's ring: halves of 64 D bytes, D / 16 DMAs of 1 KB each.  Four (D = 128) or
+// eight fill a CU's 160 KB.
 template <int D>
 struct Ring {
   static constexpr int kHalf = D * kKeyBlock;
   static constexpr int kOps = D / 16;
-  static constexpr int kSlots = D == 128 ? 5 : 8;
+  static constexpr int kSlots = 5;
 };
 
 typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
@@ -233,10 +232,24 @@ __device__ __forceinline__ bool fold_block(Wave8<RB, D>& w, const unsigned char*
 #pragma unroll
     for (int i = 0; i < kAhead && i < D / 16; ++i) v_in[i] = *reinterpret_cast<const u32x2*>(vp + i * 1024 + 8 * hf);
     half_max<RB>(sc, mx);
-    bool grow = false;
+    bool grow = false, fresh = false;
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) grow |= mx[rb] * scale_log2 > (w.m[rb] > kNegBig ? kGrowLog2 : kNegBig);
+    for (int rb = 0; rb < RB; ++rb) {
+      grow |= w.m[rb] > kNegBig && mx[rb] * scale_log2 > kGrowLog2;
+      fresh |= !(w.m[rb] > kNegBig) && mx[rb] > kNegBig;
+    }
     if (__builtin_expect(__ballot(grow) != 0, 0)) return false;
+    if (__builtin_expect(__ballot(fresh) != 0, 0)) {  // rows' first keys: their maximum is the reference
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        const bool set = !(w.m[rb] > kNegBig) && mx[rb] > kNegBig;
+        w.m[rb] = set ? mx[rb] : w.m[rb];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) sc[rb][t][r] -= set ? mx[rb] : 0.f;
+      }
+    }
     // P in bfloat16, as the products take it; the sum adds the rounded values,
     // so that the weights that O accumulates sum to one.
     bf16x8 pf[RB];
@@ -333,15 +346,12 @@ void kv8_attn_kernel(AttnShape s, AttnBatch bt, Kv8Pool pool, int nchunks, const
   if (item >= nchunks * s.Hkv) return;
   const int head = item % s.Hkv;
   const int c = item / s.Hkv;
-  int lo = 0, hi = bt.nreq - 1;  // the largest request with chunk_prefix <= c
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (bt.chunk_prefix[mid] <= c) lo = mid; else hi = mid - 1;
-  }
-  lo = __builtin_amdgcn_readfirstlane(lo);
+  // The largest request with chunk_prefix <= c: one load, a request per lane.
+  const int prefix = lane < bt.nreq ? bt.chunk_prefix[lane] : INT32_MAX;
+  const int lo = __popcll(__ballot(prefix <= c)) - 1;
   const int req = bt.req0 + lo;
-  const int end = __builtin_amdgcn_readfirstlane(bt.kv_len[lo]), first = end - s.G;
-  const int key_begin = (c - __builtin_amdgcn_readfirstlane(bt.chunk_prefix[lo])) * s.chunk_keys;
+  const int end = bt.kv_len[lo], first = end - s.G;
+  const int key_begin = (c - __builtin_amdgcn_readlane(prefix, lo)) * s.chunk_keys;
   const int key_end = min(key_begin + s.chunk_keys, end);
   const int ntiles = (key_end - key_begin + kKeyBlock - 1) / kKeyBlock;
   const int blk0 = key_begin / kKeyBlock;
@@ -387,7 +397,9 @@ void kv8_attn_kernel(AttnShape s, AttnBatch bt, Kv8Pool pool, int nchunks, const
   fill();
 
   Wave8<RB, D> w;
-  const uint64_t masks = position_mask(bt.parent != nullptr ? bt.parent + (int64_t)req * (s.G - 1) : nullptr, s.G);
+  const int whole = min(max((first + 1 - key_begin) / kKeyBlock, 0), ntiles);  // blocks that every row sees whole
+  uint64_t masks = 0;
+  if (whole < ntiles) masks = position_mask(bt.parent != nullptr ? bt.parent + (int64_t)req * (s.G - 1) : nullptr, s.G);
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
     const int row = (rg * RB + rb) * 16 + lr;
@@ -404,17 +416,12 @@ void kv8_attn_kernel(AttnShape s, AttnBatch bt, Kv8Pool pool, int nchunks, const
   auto pow2 = [&](int bytes, int t) {
     return __uint_as_float((uint32_t)__builtin_amdgcn_readlane(bytes, t) << 23);
   };
-  const int whole = min(max((first + 1 - key_begin) / kKeyBlock, 0), ntiles);  // blocks that every row sees whole
-  int from = 0, to = 1;  // blocks whose maxima are taken before the next fold
+  int from = ntiles;  // the block from which on maxima are taken before the next fold
   for (;;) {
-    for (int t = from; t < to; ++t) {
-      if (from == 0) {
-        wait_half(0);
-      } else {
-        fetch(2 * t, 0, 0, R::kOps);
-        wait_vmcnt<0>();
-        asm volatile("" ::: "memory");
-      }
+    for (int t = from; t < ntiles; ++t) {
+      fetch(2 * t, 0, 0, R::kOps);
+      wait_vmcnt<0>();
+      asm volatile("" ::: "memory");
       float zero[RB];
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) zero[rb] = 0.f;
@@ -432,7 +439,7 @@ void kv8_attn_kernel(AttnShape s, AttnBatch bt, Kv8Pool pool, int nchunks, const
       }
       lds_wait();  // read before the next DMA overwrites it
     }
-    if (from > 0) fill();
+    if (from < ntiles) fill();
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
       w.l[rb] = 0.f;
@@ -466,7 +473,6 @@ void kv8_attn_kernel(AttnShape s, AttnBatch bt, Kv8Pool pool, int nchunks, const
     for (; t < ntiles && done; ++t) step(t, Kind<true>());
     if (done) break;
     from = t - 1;
-    to = ntiles;
     wait_vmcnt<0>();
     lds_wait();
   }
@@ -565,6 +571,10 @@ int blocks_of(int rows) {
   return ((rows + 15) / 16 + g - 1) / g;
 }
 
+// Workgroups (one wave, one item each) that run at once: what LDS holds, and at
+// head dimension 64 the registers of up to three blocks.
+int64_t places(int rows, int D) { return cu_count() * (D == 64 && blocks_of(rows) <= 3 ? 8 : 4); }
+
 }  // namespace
 
 AttnShape kv8_shape(int G, int Hq, int Hkv, int D, float scale, const int32_t* kv_len, int B) {
@@ -578,10 +588,12 @@ AttnShape kv8_shape(int G, int Hq, int Hkv, int D, float scale, const int32_t* k
   s.row_groups = row_groups(s.rows);
   s.scale_log2 = scale * kLog2e;
   // For one to four rounds of items over the CUs' places the shortest chunk that
-  // fits them; of these the one with the least rounds x (chunk + an item's start:
-  // rows, pages, first block, partial, in keys).  More items than four rounds
-  // only with the longest chunk: the workspace holds no more partials.
-  const int64_t slots = cu_count() * kItems;
+  // fits them; of these the one that is done first.  One round takes a chunk and
+  // an item's start (rows, pages, first block, partial, in keys); items in more
+  // rounds are handed out as places come free, and the last ones end half a
+  // chunk apart.  More items than four rounds only with the longest chunk: the
+  // workspace holds no more partials.
+  const int64_t slots = places(s.rows, D);
   const int64_t start = 192 + 2 * s.rows;
   auto items = [&](int tiles) {
     const int keys = tiles * kKeyBlock;
@@ -589,6 +601,7 @@ AttnShape kv8_shape(int G, int Hq, int Hkv, int D, float scale, const int32_t* k
     for (int b = 0; b < B; ++b) n += (kv_len[b] + keys - 1) / keys;
     return n * Hkv * s.row_groups;
   };
+  const int64_t total = items(1) * kKeyBlock;
   int64_t best = INT64_MAX;
   int most = kMaxTiles;
   s.chunk_keys = kMaxTiles * kKeyBlock;
@@ -599,7 +612,8 @@ AttnShape kv8_shape(int G, int Hq, int Hkv, int D, float scale, const int32_t* k
       const int mid = (lo + hi) / 2;
       if (items(mid) <= r * slots) hi = mid; else lo = mid + 1;
     }
-    const int64_t cost = r * (int64_t(lo) * kKeyBlock + start);
+    const int64_t keys = int64_t(lo) * kKeyBlock;
+    const int64_t cost = r == 1 ? keys + start : (total + items(lo) * start) / slots + keys / 2;
     if (cost < best) {
       best = cost;
       s.chunk_keys = lo * kKeyBlock;
@@ -610,9 +624,8 @@ AttnShape kv8_shape(int G, int Hq, int Hkv, int D, float scale, const int32_t* k
   return s;
 }
 
-int64_t kv8_max_chunks(int Hkv, int B, int64_t max_kv_len) {
-  const int64_t slots = cu_count() * kItems;
-  const int64_t most = 4 * slots / Hkv;
+int64_t kv8_max_chunks(int rows, int Hkv, int D, int B, int64_t max_kv_len) {
+  const int64_t most = 4 * places(rows, D) / Hkv;
   const int64_t at_longest = B * ((max_kv_len + kMaxTiles * kKeyBlock - 1) / (kMaxTiles * kKeyBlock));
   return most > at_longest ? most : at_longest;
 }
