@@ -1,17 +1,23 @@
 // Appending key and value rows to a paged 8-bit cache (gfx950).
 //
-// One workgroup per (64-key block that a request's new rows touch, KV head, K
-// or V): the block's scale needs the largest magnitude of all its new rows, and
-// a block is the unit that is rewritten when its scale grows.  Scales are
-// powers of two: an e4m3 code keeps its three fraction bits under any of them,
-// so a finer scale would buy no precision, and a block whose scale grows is
-// rewritten exactly (values that leave the normal range apart).
+// The unit of work is a (64-key block that a request's new rows touch, KV head, K or
+// V): the block's scale needs the largest magnitude of all its new rows, and a block
+// is what is rewritten when its scale grows.  Scales are powers of two: an e4m3 code
+// keeps its three fraction bits under any of them, so a finer scale would buy no
+// precision, and a block whose scale grows is rewritten exactly (values that leave the
+// normal range apart).
 //
-// A thread holds four consecutive keys by eight columns, read once with 16-byte
-// loads (the 16 threads of a quad of keys read whole rows).  Codes go to an
-// LDS image of the block in its layout and from there to the pool 16 bytes at
-// a time; blocks that also hold earlier or later bytes merge them there.  Bound
-// by memory: bf16 rows read 2 bytes and write 1 per element.
+// A thread holds four consecutive keys by eight columns, read once with 16-byte loads
+// (the threads of a quad of keys read whole rows).
+//  * Prompts: a workgroup takes a unit.  Codes go to an LDS image of the block in its
+//    layout and from there to the pool 16 bytes at a time, only the pieces that hold
+//    new keys (or, where the scale grew, earlier ones); pieces of V that hold others
+//    too are read with the rows and merged.  Bound by memory, 2 bytes read and 1
+//    written per bf16 element: 8 prompts of 1 to 6,001 rows and 8 heads take 34 us,
+//    4.3 TB/s, a large copy's rate being 4.8.
+//  * Steps of a few keys: a wave takes a unit, so that all units of a large batch are
+//    resident at once, and stores its codes straight away.  Bound by the latency of
+//    table, rows and store, one behind the other: 10 us for 64 requests of 5 keys.
 #include "fp8.h"
 
 namespace sdv {
@@ -19,6 +25,10 @@ namespace sdv {
 namespace {
 
 constexpr int kAppendThreads = 256;
+// New keys per request up to which a wave takes a unit: at head dimension 128 its
+// 16 threads per row hold four quads of keys.  64 requests of 5 keys and 32 heads:
+// 21.5 us with a workgroup per unit, 10.0 with a wave.
+constexpr int kFewKeys = 13;
 constexpr int kLowestExp = 27;  // byte of the smallest scale, 2^-100
 
 // Smallest e with most <= 448 * 2^e as a scale byte, at least 2^-100 (most
@@ -67,137 +77,262 @@ __device__ __forceinline__ uint32_t first_bytes(int n) {
   return n >= 4 ? 0xffffffffu : n <= 0 ? 0u : (1u << (8 * n)) - 1u;
 }
 
-template <typename T, int D>
-__global__ __launch_bounds__(kAppendThreads)
-void kv8_append_kernel(Kv8Append a, Kv8Pool pool, int Hkv, const T* __restrict__ k_new, int64_t k_stride,
-                       const T* __restrict__ v_new, int64_t v_stride) {
-  constexpr int TPR = D / 8;                       // threads per row
-  constexpr int kQuads = kAppendThreads / TPR;     // quads of keys in flight at once
-  constexpr int kRounds = 16 / kQuads < 1 ? 1 : 16 / kQuads;
-  constexpr int kPieces = D * kKeyBlock / 16;      // 16-byte pieces of a block
-  __shared__ __align__(16) uint32_t image[D * kKeyBlock / 4];
-  __shared__ float wave_most[kAppendThreads / kWave];
+// One (block, head, K or V) that takes new keys.
+struct Unit {
+  u32x4* block;
+  uint8_t* scale;
+  int b0, e0;    // keys b0 .. e0 - 1 of the block are new
+  int64_t row0;  // row of the new tensors for key 0 of the block
+  int head;
+  bool is_v;
+};
 
-  const int c = blockIdx.x, head = blockIdx.y, t = threadIdx.x;
-  const bool is_v = blockIdx.z != 0;
-  int lo = 0, hi = a.nreq - 1;  // the largest request with blk_prefix <= c
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (a.blk_prefix[mid] <= c) lo = mid; else hi = mid - 1;
-  }
+template <int D>
+__device__ __forceinline__ Unit unit_of(const Kv8Append& a, const Kv8Pool& pool, int Hkv, int unit, int lane) {
+  Unit u;
+  u.is_v = (unit & 1) != 0;
+  u.head = (unit >> 1) % Hkv;
+  const int c = (unit >> 1) / Hkv;
+  // The largest request with blk_prefix <= c: one load, a request per lane.
+  const int prefix = lane < a.nreq ? a.blk_prefix[lane] : INT32_MAX;
+  const int lo = __popcll(__ballot(prefix <= c)) - 1;
   const int end = a.kv_len[lo], begin = end - a.new_len[lo];
-  const int blk = begin / kKeyBlock + (c - a.blk_prefix[lo]);
+  const int blk = begin / kKeyBlock + (c - __builtin_amdgcn_readlane(prefix, lo));
   const int key0 = blk * kKeyBlock;
   const int per_page_shift = pool.page_shift - 6;
   int page = pool.table[(int64_t)a.req[lo] * pool.max_pages + (blk >> per_page_shift)];
   page = min(max(page, 0), pool.num_pages - 1);
-  const int64_t at = ((((int64_t)page * Hkv + head) << per_page_shift)) + (blk & ((1 << per_page_shift) - 1));
-  uint8_t* scale = (is_v ? pool.v_scale : pool.k_scale) + at;
-  u32x4* block = reinterpret_cast<u32x4*>((is_v ? pool.v : pool.k) + at * (D * kKeyBlock));
+  const int64_t at = ((((int64_t)page * Hkv + u.head) << per_page_shift)) + (blk & ((1 << per_page_shift) - 1));
+  u.scale = (u.is_v ? pool.v_scale : pool.k_scale) + at;
+  u.block = reinterpret_cast<u32x4*>((u.is_v ? pool.v : pool.k) + at * (D * kKeyBlock));
+  u.b0 = max(begin - key0, 0);
+  u.e0 = min(end - key0, kKeyBlock);
+  u.row0 = a.new_off[lo] + (key0 - begin);
+  return u;
+}
 
-  const bool has_old = begin > key0;                       // earlier keys stay in this block
-  const bool whole = !has_old && end >= key0 + kKeyBlock;  // every byte is new
-  const int was = has_old ? *scale : 0;
-  u32x4 there[kPieces / kAppendThreads];  // what a partly written block holds, read with the rows
-  if (!whole) {
+// Rows 4 quad .. + 3 of the block, 8 columns from col; zeros where no key is new (a
+// new row is read in its place, so that the four loads are on their way together).
+// Returns the largest finite magnitude.
+template <typename T>
+__device__ __forceinline__ float load_quad(const Unit& u, const T* src, int64_t stride, int quad, int col,
+                                           float (&x)[4][8]) {
 #pragma unroll
-    for (int i = 0; i < kPieces / kAppendThreads; ++i) there[i] = block[t + i * kAppendThreads];
-  }
-
-  const T* src = is_v ? v_new : k_new;
-  const int64_t stride = is_v ? v_stride : k_stride;
-  const int col = (t % TPR) * 8;
-  float x[kRounds][4][8];
+  for (int r = 0; r < 4; ++r)
+    load_row8(src + (u.row0 + min(max(4 * quad + r, u.b0), u.e0 - 1)) * stride + col, x[r]);
   float most = 0.f;
 #pragma unroll
-  for (int n = 0; n < kRounds; ++n)
+  for (int r = 0; r < 4; ++r) {
+    const bool is_new = 4 * quad + r >= u.b0 && 4 * quad + r < u.e0;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int key = key0 + 4 * (t / TPR + n * kQuads) + r;
-      const bool is_new = t / TPR + n * kQuads < 16 && key >= begin && key < end;
-      if (is_new) {
-        load_row8(src + (a.new_off[lo] + (key - begin)) * stride + head * D + col, x[n][r]);
-      } else {
+    for (int e = 0; e < 8; ++e) x[r][e] = is_new ? x[r][e] : 0.f;
+  }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[n][r][e] = 0.f;
-      }
+  for (int r = 0; r < 4; ++r)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float m = fabsf(x[r][e]);
+      most = m < INFINITY ? fmaxf(most, m) : most;  // infinities and NaN do not set the scale
     }
+  return most;
+}
+
+// Index of the dword that holds columns col .. + 3 of a key in a block of K, and of
+// the one that holds keys 4 quad .. + 3 of column d in a block of V.
+__device__ __forceinline__ int k_dword(int key, int col) {
+  // [D/64][4 t][4 g][16 r][16 b]
+  return (((col / 64 * 4 + key / 16) * 4 + col % 64 / 16) * 16 + key % 16) * 4 + col % 16 / 4;
+}
+__device__ __forceinline__ int v_dword(int quad, int d) {
+  // [D/16][4 g][16 d][4 t][4 r]
+  return ((d / 16 * 4 + quad % 4) * 16 + d % 16) * 4 + quad / 4;
+}
+
+__device__ __forceinline__ u32x2 encode8(const float (&x)[8], float mul) {
+  return u32x2{encode4(x[0] * mul, x[1] * mul, x[2] * mul, x[3] * mul),
+               encode4(x[4] * mul, x[5] * mul, x[6] * mul, x[7] * mul)};
+}
+
+// A wave per unit, for at most kFewKeys new keys of a request: the quads that they
+// lie in are one round of loads, and each thread stores its own codes where they
+// belong.  Nothing of the block is read but the dwords of V that hold other keys too,
+// unless the scale grows.
+template <typename T, int D>
+__global__ __launch_bounds__(kAppendThreads)
+void kv8_append_few_kernel(Kv8Append a, Kv8Pool pool, int Hkv, int nunits, const T* __restrict__ k_new,
+                           int64_t k_stride, const T* __restrict__ v_new, int64_t v_stride) {
+  constexpr int TPR = D / 8;  // threads per row
+  static_assert(kWave / TPR * 4 >= kFewKeys + 3, "one round of loads");
+  constexpr int kPieces = D * kKeyBlock / 16;  // 16-byte pieces of a block
+  const int unit = blockIdx.x * (kAppendThreads / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (unit >= nunits) return;
+  const int lane = threadIdx.x & 63;
+  const Unit u = unit_of<D>(a, pool, Hkv, unit, lane);
+  const int col = lane % TPR * 8, quad = u.b0 / 4 + lane / TPR;
+  const bool mine = 4 * quad < u.e0;
+  const int was = u.b0 > 0 ? *u.scale : 0;
+  uint32_t* const words = reinterpret_cast<uint32_t*>(u.block);
+  // Bytes of the quad's dwords of V that are new, and earlier keys.
+  const uint32_t old_bytes = first_bytes(u.b0 - 4 * quad);
+  const uint32_t new_bytes = first_bytes(u.e0 - 4 * quad) & ~old_bytes;
+  uint32_t there[8];
 #pragma unroll
-  for (int n = 0; n < kRounds; ++n)
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
+  for (int e = 0; e < 8; ++e)
+    there[e] = u.is_v && mine && new_bytes != 0xffffffffu ? words[v_dword(quad, col + e)] : 0u;
+  float x[4][8];
+  const float most = wave_max(
+      load_quad(u, (u.is_v ? v_new : k_new) + u.head * D, u.is_v ? v_stride : k_stride, quad, col, x));
+  const int now = max(scale_byte(most), was);
+  const float mul = pow2_f32(127 - now);
+  const bool grew = u.b0 > 0 && now > was;
+  const float shrink = pow2_f32(max(was - now, -126));
+  if (mine) {
+    if (u.is_v) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float m = fabsf(x[n][r][e]);
-        most = m < INFINITY ? fmaxf(most, m) : most;  // infinities and NaN do not set the scale
+        const uint32_t codes = encode4(x[0][e] * mul, x[1][e] * mul, x[2][e] * mul, x[3][e] * mul);
+        const uint32_t old = grew ? rescale4(there[e], shrink) : there[e];
+        words[v_dword(quad, col + e)] =
+            (codes & new_bytes) | (old & old_bytes) | (there[e] & ~(new_bytes | old_bytes));
       }
-  most = wave_max(most);
-  if ((t & 63) == 0) wave_most[t >> 6] = most;
+    } else {
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (4 * quad + r >= u.b0 && 4 * quad + r < u.e0)
+          *reinterpret_cast<u32x2*>(words + k_dword(4 * quad + r, col)) = encode8(x[r], mul);
+    }
+  }
+  // The other earlier keys, each dword by one thread: those of V below the first quad.
+  if (grew) {
+    for (int p = lane; p < kPieces; p += kWave) {
+      const u32x4 old = u.block[p];
+      if (!u.is_v) {
+        if (p / 64 % 4 * 16 + p % 16 < u.b0)
+          u.block[p] = u32x4{rescale4(old[0], shrink), rescale4(old[1], shrink), rescale4(old[2], shrink),
+                             rescale4(old[3], shrink)};
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (4 * j + p / 16 % 4 < u.b0 / 4) words[4 * p + j] = rescale4(old[j], shrink);
+      }
+    }
+  }
+  if (lane == 0) *u.scale = (uint8_t)now;
+}
+
+// A workgroup per unit: the new codes are laid out in LDS and the touched pieces of
+// the block written whole.
+template <typename T, int D>
+__global__ __launch_bounds__(kAppendThreads)
+void kv8_append_kernel(Kv8Append a, Kv8Pool pool, int Hkv, const T* __restrict__ k_new, int64_t k_stride,
+                       const T* __restrict__ v_new, int64_t v_stride) {
+  constexpr int TPR = D / 8;  // threads per row
+  constexpr int kQuads = kAppendThreads / TPR;
+  static_assert(kQuads * 4 >= kKeyBlock, "one round of loads");
+  constexpr int kPieces = D * kKeyBlock / 16;  // 16-byte pieces of a block
+  constexpr int kMine = kPieces / kAppendThreads;
+  __shared__ __align__(16) uint32_t image[D * kKeyBlock / 4];
+  __shared__ float wave_most[kAppendThreads / kWave];
+
+  const int t = threadIdx.x, lane = t & 63;
+  const Unit u = unit_of<D>(a, pool, Hkv, blockIdx.x, lane);
+  const int b0 = u.b0, e0 = u.e0;
+  const bool is_v = u.is_v;
+  u32x4* const block = u.block;
+
+  // Keys of the block that are new, and earlier ones that stay in it.
+  const uint64_t old_keys = b0 > 0 ? ~0ull >> (64 - b0) : 0ull;
+  const uint64_t new_keys = (~0ull >> (64 - e0)) & ~old_keys;
+  const int was = b0 > 0 ? *u.scale : 0;
+  // A piece of 16 bytes holds one key's columns of K, a column of 16 keys of V.
+  // Those of V that hold other keys beside new ones are read with the rows.
+  auto keys_of = [&](int p) {
+    return is_v ? 0x000f000f000f000full << (4 * (p / 16 % 4)) : 1ull << (16 * (p / 64 % 4) + p % 16);
+  };
+  u32x4 there[kMine];
+#pragma unroll
+  for (int i = 0; i < kMine; ++i) {
+    const int p = t + i * kAppendThreads;
+    const uint64_t keys = keys_of(p);
+    there[i] = u32x4{0u, 0u, 0u, 0u};
+    if ((keys & new_keys) != 0 && (keys & ~new_keys) != 0) there[i] = block[p];
+  }
+
+  const int col = t % TPR * 8, quad = t / TPR;  // keys 4 quad .. + 3 of the block
+  float x[4][8];
+  float most = wave_max(load_quad(u, (is_v ? v_new : k_new) + u.head * D, is_v ? v_stride : k_stride, quad, col, x));
+  if (lane == 0) wave_most[t >> 6] = most;
   __syncthreads();
   most = fmaxf(fmaxf(wave_most[0], wave_most[1]), fmaxf(wave_most[2], wave_most[3]));
   const int now = max(scale_byte(most), was);
   const float mul = pow2_f32(127 - now);
 
+  if (quad < kKeyBlock / 4) {
+    if (is_v) {
 #pragma unroll
-  for (int n = 0; n < kRounds; ++n) {
-    const int quad = t / TPR + n * kQuads;
-    if (quad < 16) {
-      const int kt = quad >> 2, kg = quad & 3;
-      if (is_v) {
-        // [D/16][4 g][16 d][4 t][4 r]: the four keys of a quad are one dword.
+      for (int e = 0; e < 8; ++e)
+        image[v_dword(quad, col + e)] = encode4(x[0][e] * mul, x[1][e] * mul, x[2][e] * mul, x[3][e] * mul);
+    } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int d = col + e;
-          image[((d / 16 * 4 + kg) * 16 + d % 16) * 4 + kt] =
-              encode4(x[n][0][e] * mul, x[n][1][e] * mul, x[n][2][e] * mul, x[n][3][e] * mul);
-        }
-      } else {
-        // [D/64][4 t][4 g][16 r][16 b]
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int p = (((col / 64 * 4 + kt) * 4 + col % 64 / 16) * 16 + kg * 4 + r) * 4 + col % 16 / 4;
-          *reinterpret_cast<u32x2*>(image + p) =
-              u32x2{encode4(x[n][r][0] * mul, x[n][r][1] * mul, x[n][r][2] * mul, x[n][r][3] * mul),
-                    encode4(x[n][r][4] * mul, x[n][r][5] * mul, x[n][r][6] * mul, x[n][r][7] * mul)};
-        }
-      }
+      for (int r = 0; r < 4; ++r)
+        *reinterpret_cast<u32x2*>(image + k_dword(4 * quad + r, col)) = encode8(x[r], mul);
     }
   }
   __syncthreads();
-  const bool grew = has_old && now > was;
+  // A grown scale rewrites the earlier keys too.
+  const bool grew = b0 > 0 && now > was;
   const float shrink = pow2_f32(max(was - now, -126));
 #pragma unroll
-  for (int i = 0; i < kPieces / kAppendThreads; ++i) {
+  for (int i = 0; i < kMine; ++i) {
     const int p = t + i * kAppendThreads;
+    const uint64_t keys = keys_of(p);
     u32x4 r = reinterpret_cast<const u32x4*>(image)[p];
-    if (!whole) {
+    if (grew && (keys & old_keys) != 0) {
+      there[i] = block[p];
+    } else if ((keys & new_keys) == 0) {
+      continue;
+    }
+    if ((keys & ~new_keys) != 0) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        // Keys of dword j: one key's four columns of K, four keys of V.
-        const int key = is_v ? key0 + 16 * j + 4 * (p / 16 % 4) : key0 + 16 * (p / 64 % 4) + p % 16;
-        const uint32_t before = is_v ? first_bytes(begin - key) : begin > key ? 0xffffffffu : 0u;
-        const uint32_t upto = is_v ? first_bytes(end - key) : end > key ? 0xffffffffu : 0u;
+        const int key = is_v ? 16 * j + 4 * (p / 16 % 4) : 16 * (p / 64 % 4) + p % 16;
+        const uint32_t before = is_v ? first_bytes(b0 - key) : b0 > key ? 0xffffffffu : 0u;
+        const uint32_t upto = is_v ? first_bytes(e0 - key) : e0 > key ? 0xffffffffu : 0u;
         const uint32_t old = grew ? rescale4(there[i][j], shrink) : there[i][j];
         r[j] = (old & before) | (r[j] & upto & ~before) | (there[i][j] & ~upto);
       }
     }
     block[p] = r;
   }
-  if (t == 0) *scale = (uint8_t)now;
+  if (t == 0) *u.scale = (uint8_t)now;
 }
 
 }  // namespace
 
 hipError_t launch_kv8_append(const Kv8Append& a, const Kv8Pool& pool, int Hkv, int D, bool f32, const void* k_new,
                              int64_t k_stride, const void* v_new, int64_t v_stride, hipStream_t stream) {
-  const dim3 grid(a.blk_prefix[a.nreq], Hkv, 2);
+  const int nunits = a.blk_prefix[a.nreq] * Hkv * 2;
+  int most = 0;
+  for (int i = 0; i < a.nreq; ++i) most = most > a.new_len[i] ? most : a.new_len[i];
+  const bool few = most <= kFewKeys;
+  const int per = few ? kAppendThreads / kWave : 1;
+  const dim3 grid((nunits + per - 1) / per), block(kAppendThreads);
 #define SDV_APPEND(T, DIM)                                                                                       \
-  hipLaunchKernelGGL((kv8_append_kernel<T, DIM>), grid, dim3(kAppendThreads), 0, stream, a, pool, Hkv,            \
-                     static_cast<const T*>(k_new), k_stride, static_cast<const T*>(v_new), v_stride)
-  if (f32 && D == 128) SDV_APPEND(float, 128);
-  else if (f32) SDV_APPEND(float, 64);
-  else if (D == 128) SDV_APPEND(uint16_t, 128);
-  else SDV_APPEND(uint16_t, 64);
+  if (few)                                                                                                       \
+    hipLaunchKernelGGL((kv8_append_few_kernel<T, DIM>), grid, block, 0, stream, a, pool, Hkv, nunits,             \
+                       static_cast<const T*>(k_new), k_stride, static_cast<const T*>(v_new), v_stride);          \
+  else                                                                                                           \
+    hipLaunchKernelGGL((kv8_append_kernel<T, DIM>), grid, block, 0, stream, a, pool, Hkv,                         \
+                       static_cast<const T*>(k_new), k_stride, static_cast<const T*>(v_new), v_stride)
+  if (f32 && D == 128) {
+    SDV_APPEND(float, 128);
+  } else if (f32) {
+    SDV_APPEND(float, 64);
+  } else if (D == 128) {
+    SDV_APPEND(uint16_t, 128);
+  } else {
+    SDV_APPEND(uint16_t, 64);
+  }
 #undef SDV_APPEND
   return hipGetLastError();
 }

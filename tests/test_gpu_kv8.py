@@ -118,6 +118,27 @@ def test_append_steps_cut_back_and_odd_values():
         c.check()
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("new", [1, 4, 13, 14])
+def test_append_steps_of_growing_rows(new, dim, dtype):
+    """Steps at every place in a block, over its end too, of rows that outgrow the earlier scale and of rows that do not."""
+    rng = np.random.default_rng(new)
+    heads = 3
+    lens = [new + i for i in range(0, 70, 3)]
+    B = len(lens)
+    c = Cache(rng, [n + 3 * new for n in lens], heads, dim, 64)
+    d = sd.Dims(B, 0, heads, heads, dim, 32, 1, 1 if dtype == torch.bfloat16 else 0, 0)
+    off = np.arange(B) * new
+    for step, size in enumerate((1.0, 2.0 ** -5, 37.0, 2.0 ** 20)):
+        x = [torch.from_numpy(rng.normal(size=(B * new, heads, dim)) * size).to(dtype) for _ in range(2)]
+        at = [n + step * new for n in lens]
+        c.append(*(a.double().numpy() for a in x), off, [new] * B, at)
+        sd.sd_kv8_append(d, c.handle, *(a.cuda() for a in x), off, [new] * B, at)
+        torch.cuda.synchronize()
+        c.check()
+
+
 # ---- attention -------------------------------------------------------------------
 
 def check_attention(got, q, seg, kv_len, heads, parent, scale, what):
@@ -207,6 +228,81 @@ def test_attention_of_large_and_growing_scores():
     got = attend(G, H, H, D, c, lens, q.cuda(), None, 1 / np.sqrt(D))
     check_attention(got, q.double().numpy(), fp8.kv8_segments(c.k, c.v, c.ks, c.vs, c.table, lens), lens, H, None,
                     1 / np.sqrt(D), "growing scores")
+
+
+@pytest.mark.parametrize("G,Hq,Hkv,D,page,tree", [
+    (1, 16, 16, 128, 64, False), (5, 16, 16, 128, 64, False), (5, 8, 8, 64, 128, False), (9, 32, 4, 128, 256, False),
+    (11, 32, 4, 128, 64, False), (16, 32, 4, 64, 64, True)])
+def test_attention_of_long_chunks(G, Hq, Hkv, D, page, tree):
+    """So many sequences that a wave folds many blocks of one: lengths from a few keys to 1,500."""
+    rng = np.random.default_rng(G + D)
+    lens = [1500 - 53 * i if i < 24 else G + 61 * (i - 24) for i in range(28)]
+    c = filled(rng, lens, Hkv, D, page)
+    q = torch.from_numpy(rng.normal(size=(len(lens), G, Hq, D)) * 2).bfloat16()
+    parent = pd = None
+    if tree:
+        parent = np.maximum(np.arange(G - 1)[None, :] - rng.integers(1, 5, (len(lens), G - 1)), -1).astype(np.int32)
+        pd = torch.from_numpy(parent).cuda()
+    got = attend(G, Hq, Hkv, D, c, lens, q.cuda(), pd, 1 / np.sqrt(D))
+    seg = fp8.kv8_segments(c.k, c.v, c.ks, c.vs, c.table, lens)
+    worst = check_attention(got, q.double().numpy(), seg, lens, Hkv, parent, 1 / np.sqrt(D), "long chunks")
+    announce(f"kv8 attention of long chunks G {G} D {D}: {worst:.2f} of the bound")
+
+
+@pytest.mark.parametrize("G,Hq,Hkv,D", [(2, 16, 16, 128), (5, 16, 16, 64), (10, 32, 4, 128)])
+def test_attention_of_scores_that_jump(G, Hq, Hkv, D):
+    """Scores rise and fall by hundreds from one stretch of keys to the next, inside
+    a wave's share too.  One column alone makes a score, so it is one product: exact in
+    float32 but for the factors scale and log2 e, under 3 * 2^-24 * 300 = 5e-5 of p, within the bound's twentieth
+    (2^-8 / 20 = 2e-4)."""
+    rng = np.random.default_rng(G)
+    B = 24
+    lens = [1400 - 31 * i for i in range(B)]
+    total = sum(lens)
+    levels = np.array([0.0, 100.0, -200.0, 220.0, 220.0, 30.0, 290.0, 0.0])
+    x = [rng.normal(size=(total, Hkv, D)) for _ in range(2)]
+    x[0][...] = 0.0
+    off = np.cumsum([0] + lens[:-1])
+    for o, n in zip(off, lens):
+        stretch = (np.arange(n) + rng.integers(0, 300)) // 150 % len(levels)
+        x[0][o:o + n, :, 0] = levels[stretch][:, None] + rng.normal(size=(n, Hkv))
+    c = Cache(rng, lens, Hkv, D, 64)
+    c.append(*x, off, lens, lens)
+    c.upload()
+    q = torch.zeros((B, G, Hq, D), dtype=torch.bfloat16)
+    q[..., 0] = torch.from_numpy(rng.choice([1.0, -1.0, 0.5], (B, G, Hq))).bfloat16()
+    got = attend(G, Hq, Hkv, D, c, lens, q.cuda(), None, 1.0)
+    seg = fp8.kv8_segments(c.k, c.v, c.ks, c.vs, c.table, lens)
+    check_attention(got, q.double().numpy(), seg, lens, Hkv, None, 1.0, "scores that jump")
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_nan_at_the_end_of_a_long_chunk(D):
+    rng = np.random.default_rng(D)
+    B, G, H = 24, 5, 16
+    lens = [1300 - 29 * i for i in range(B)]
+    off = np.cumsum([0] + lens[:-1])
+    x = [rng.normal(size=(sum(lens), H, D)) for _ in range(2)]
+    clean = [a.copy() for a in x]
+    x[1][off[3] + lens[3] - G + 2, :, 7] = np.nan   # a value that positions 2 .. see
+    x[0][off[9] + lens[9] - G + 4, :, 5] = np.nan   # a key that the last one sees
+    x[1][off[11] + 700, 4, 9] = np.nan              # a value in the middle: its head and column alone
+    c = Cache(rng, lens, H, D, 64)
+    c.append(*x, off, lens, lens)
+    c.upload()
+    q = torch.from_numpy(rng.normal(size=(B, G, H, D))).bfloat16()
+    got = attend(G, H, H, D, c, lens, q.cuda(), None, 1 / np.sqrt(D))
+    assert np.isnan(got[3, 2:, :, 7]).all() and np.isnan(got[9, 4]).all() and np.isnan(got[11, :, 4, 9]).all()
+    c.append(*clean, off, lens, lens)
+    ref = verify_attention(q.double().numpy(), *fp8.kv8_segments(c.k, c.v, c.ks, c.vs, c.table, lens), lens, H)
+    for b in range(B):
+        if b in (3, 9, 11):
+            first = {3: 2, 9: 4, 11: 0}[b]
+            assert np.isfinite(got[b, :first]).all()
+            assert np.abs(got[b, :first] - ref[b, :first]).max(initial=0) < 0.1 * np.abs(ref).max()
+        else:
+            assert np.isfinite(got[b]).all()
+            assert np.abs(got[b] - ref[b]).max() < 0.02 * np.abs(ref).max()
 
 
 @pytest.mark.parametrize("G,Hq,Hkv,D", [(4, 2, 1, 128), (4, 1, 1, 64), (9, 8, 1, 128)])
