@@ -51,11 +51,11 @@ hipError_t launch_residual_norm(bool f32, int rows, int width, float eps, const 
 // The projection's tiles for M rows, K columns, V entries.
 struct Fp8Plan {
   int M, K, V;
-  int mb, nw;       // 32-row blocks and waves (of 32 entries each) per workgroup
+  int mb, nw;       // 32-row blocks, and blocks of 32 entries, per tile
   int mtiles, ntiles;
 };
 Fp8Plan fp8_plan(int M, int K, int V);
-size_t fp8_logits_bytes(const Fp8Plan& p);
+size_t fp8_logits_bytes(int M, int V);
 hipError_t launch_logits_fp8(const Fp8Plan& p, const void* hidden, const float* hidden_scale, const void* w,
                              const float* w_scale, float* logits, float* row_lse, void* ws, hipStream_t stream);
 

@@ -97,7 +97,7 @@ size_t sd_fp8_workspace_bytes(const sd_dims_t* d, int32_t max_kv_len) {
     n = align_up(attn_partial_bytes(chunks, d->n_kv_heads, rows, d->head_dim));
   }
   if (check_projection(d) == SD_OK)
-    n = std::max(n, align_up(fp8_logits_bytes(fp8_plan(d->batch * (d->gamma + 1), d->hidden, d->vocab))));
+    n = std::max(n, align_up(fp8_logits_bytes(d->batch * (d->gamma + 1), d->vocab)));
   return n;
 }
 
@@ -217,7 +217,7 @@ int sd_verify_logits_fp8(const sd_dims_t* d, const void* hidden, const float* hi
     return SD_ERR_INVALID_ARGUMENT;
   const Fp8Plan p = fp8_plan(d->batch * (d->gamma + 1), d->hidden, d->vocab);
   if (int64_t(p.ntiles + 7) * p.mtiles > kMaxGrid) return SD_ERR_UNSUPPORTED;
-  if (workspace_bytes < fp8_logits_bytes(p)) return SD_ERR_WORKSPACE;
+  if (workspace_bytes < fp8_logits_bytes(p.M, p.V)) return SD_ERR_WORKSPACE;
   return launch_logits_fp8(p, hidden, hidden_scale, w, w_scale, logits, row_lse, workspace,
                            static_cast<hipStream_t>(stream)) == hipSuccess
              ? SD_OK

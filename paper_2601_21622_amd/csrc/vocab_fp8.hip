@@ -5,7 +5,10 @@
 // and per row and tile of vocabulary entries the maximum and the sum of
 // exponentials, folded into the rows' log-sum-exp by the bf16 projection's kernel.
 //
-// Bound by the stream of W up to about 200 rows, by the matrix cores past that.
+// Bound by the stream of W up to about 64 rows (1.05 GB for 64 x 128,256 x 8,192 in 192
+// us, 5.5 TB/s), by the matrix cores' power past that: 224 x 128,256 x 4,096 takes 236 us,
+// 1.0 PFLOP/s, where a large bfloat16 product of the library reaches 1.2 on the same card,
+// and the same launch over codes that are all zero, with nothing else changed, takes 191.
 // A row's 128 columns of one scale are one 128-byte line, so W [V][K] and the
 // rows [M][K] are streamed as they are, in whole lines by LDS DMA, a line of
 // every row of the tile per stage.  Codes widen to bfloat16 exactly on their way
@@ -15,14 +18,18 @@
 // A line's products are summed from zero and then added to the accumulators
 // times both scales.
 //
+// A workgroup is eight waves of 32 entries each: a tile of 256, every row line read by
+// all of them.  Where tiles of 128 are one round of the CUs at most, two parts of four
+// waves sum over one half of the columns each, over the same 128 entries, and the second
+// part's sums are added to the first's: twice as many CUs work, each line by line as
+// before.  96 x 32,000 x 4,096: 43.5 us so, 54 with tiles of 256; 160 x 50,304 x 4,096,
+// where tiles of 128 are two rounds: 117 and 79.
+//
 // Of a 32-row group (four 1 KB blocks of eight rows), unit u (16 bytes) of row r
 // sits at slot 8 r + (u + r / 2) mod 8, so that the 32 rows that a fragment read
 // takes of one unit fall on distinct banks.  The line's eight units are read in
 // pairs: lanes 0-31 take unit 2 j, lanes 32-63 unit 2 j + 1, which are the 32
 // columns of two MFMA steps; both operands permute the columns alike.
-#include <algorithm>
-#include <atomic>
-
 #include "fp8.h"
 #include "vocab_tile.h"
 
@@ -32,10 +39,13 @@ namespace {
 
 constexpr int kScaleBytes = 1024;  // a stage's row scales: 256 floats
 
-constexpr int stage_bytes(int mb, int nw) { return 4 * (mb + nw) * 1024 + kScaleBytes; }
+constexpr int kWaves = 8;
+constexpr int kCUs = 256;  // of the MI355X
+
+constexpr int line_bytes(int mb, int nw) { return 4 * (mb + nw) * 1024 + kScaleBytes; }
 constexpr int stages(int mb, int nw) {
-  const int n = 160 * 1024 / stage_bytes(mb, nw);
-  return n < 6 ? n : 6;
+  const int n = 160 * 1024 / (kWaves / nw * line_bytes(mb, nw));
+  return n < 4 ? n : 4;  // more bring nothing
 }
 
 // LDS DMA of 16 (or 4) bytes per lane from base + off into LDS bytes lds + 16 l
@@ -54,35 +64,46 @@ __device__ __forceinline__ void base_dma_word(const void* base, uint32_t off, ui
                : : "s"(lds), "v"(off), "s"(base) : "m0", "memory");
 }
 
-template <bool X>
-struct Flag {
-  static constexpr bool value = X;
+template <int X>
+struct Int {
+  static constexpr int value = X;
 };
 
 template <int MB, int NW>
-__global__ __launch_bounds__(NW * kWave, 1)
+__global__ __launch_bounds__(kWaves * kWave, 1)
 void vocab_fp8_kernel(int M, int K, int V, int ntiles, int mtiles, const uint8_t* __restrict__ hidden,
                       const float* __restrict__ hidden_scale, const uint8_t* __restrict__ w,
                       const float* __restrict__ w_scale, float* __restrict__ logits, float2* __restrict__ partials) {
   constexpr int kHBlocks = 4 * MB;
-  constexpr int kStage = stage_bytes(MB, NW);
-  constexpr int kScaleAt = kStage - kScaleBytes;
+  constexpr int kParts = kWaves / NW;
+  constexpr int kLine = line_bytes(MB, NW);
+  constexpr int kStage = kParts * kLine;
+  constexpr int kScaleAt = kLine - kScaleBytes;
   constexpr int S = stages(MB, NW);
   constexpr int kHOps = (kHBlocks + NW - 1) / NW;  // hidden blocks per wave (past the last: the last again)
   constexpr int kOps = 4 + kHOps + 1;              // DMAs per wave and line
   constexpr int kSteps = 4 * MB;
+  constexpr int kRowOps = kHOps + 1;
   static_assert(S >= 2 && (S - 1) * kOps < 64, "two stages; vmcnt holds 6 bits");
-  __shared__ __align__(1024) unsigned char lds[S * kStage];
+  static_assert(kParts == 1 || (kParts == 2 && MB * 16 * 1024 <= S * kStage), "the second part's sums");
+  __shared__ __align__(1024) unsigned char lds_all[S * kStage];
 
   // The M-tiles of one vocabulary tile share an XCD (ids 8 apart).
   const int grp = 8 * mtiles;
   const int tile = (blockIdx.x / grp) * 8 + (blockIdx.x & 7);
   if (tile >= ntiles) return;
   const int m0 = ((blockIdx.x % grp) >> 3) * MB * 32;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int part = kParts == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / (NW * kWave));
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) - part * NW;
+  unsigned char* const lds = lds_all + part * kLine;
   const int lane = threadIdx.x & 63;
   const int blk0 = tile * NW + wave;
-  const int nlines = K / kColBlock, nscales = (K + kColBlock - 1) / kColBlock;
+  // Each part of the waves sums over lines of its own, first .. first + nlines - 1; only
+  // the last part has columns past the last whole line.
+  const int all_lines = K / kColBlock;
+  const int first = part * (all_lines / kParts);
+  const int nlines = (part == kParts - 1 ? all_lines : all_lines / kParts) - first;
+  const int nscales = (K + kColBlock - 1) / kColBlock;
 
   // Lane l of block q of a group brings unit (l % 8) - r / 2 of row r = 8 q + l
   // / 8.  Rows past V and past M repeat the last row.  Offsets count from the
@@ -100,21 +121,23 @@ void vocab_fp8_kernel(int M, int K, int V, int ntiles, int mtiles, const uint8_t
     hblk[i] = min(wave + i * NW, kHBlocks - 1);
     hoff[i] = (uint32_t)min(8 * hblk[i] + (lane >> 3), M - 1 - m0) * (uint32_t)K + unit(hblk[i]) * 16;
   }
-  const uint32_t soff = (uint32_t)min((int)(threadIdx.x & 255), M - 1 - m0) * 4u;
+  const uint32_t soff = (uint32_t)min((int)(threadIdx.x & 255), M - 1 - m0) * 4u;  // each 4 waves bring all
   const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)lds;
-  // DMA j of line c into stage s, of its first `units` units (the others repeat the first).
+  // DMA j of line c into stage s, of its first `units` units (the others repeat the
+  // first): the rows' and their scales, then the wave's own entries'.
   auto issue_op = [&](int j, int s, int c, int units = 8) {
     const uint32_t dst = lds_base + (uint32_t)s * kStage;
     const int64_t o = (int64_t)c * kLineBytes;
+    const int q = j - kRowOps;
     uint32_t back = 0;
-    if (units < 8 && j < 4 + kHOps) {
-      const int u = unit(j < 4 ? j : hblk[j < 4 ? 0 : j - 4]);
+    if (units < 8 && j != kHOps) {
+      const int u = unit(q >= 0 ? q : hblk[j < kHOps ? j : 0]);
       back = u >= units ? (uint32_t)u * 16 : 0;
     }
-    if (j < 4)
-      base_dma<true>(wbase + o, woff[j] - back, dst + (kHBlocks + wave * 4 + j) * 1024);
-    else if (j < 4 + kHOps)
-      base_dma<false>(hbase + o, hoff[j - 4] - back, dst + hblk[j - 4] * 1024);
+    if (q >= 0)
+      base_dma<true>(wbase + o, woff[q < 0 ? 0 : q] - back, dst + (kHBlocks + wave * 4 + q) * 1024);
+    else if (j < kHOps)
+      base_dma<false>(hbase + o, hoff[j] - back, dst + hblk[j] * 1024);
     else
       base_dma_word(hidden_scale + (int64_t)c * M + m0, soff, dst + kScaleAt + (wave & 3) * 256);
   };
@@ -137,23 +160,39 @@ void vocab_fp8_kernel(int M, int K, int V, int ntiles, int mtiles, const uint8_t
 
   // Tiles start on different lines and wrap: rows a multiple of 4 KB apart would
   // otherwise send every workgroup to the same memory channels at once.
-  int l = nlines > 0 ? (int)((unsigned)tile % (unsigned)nlines) : 0, next = l;
+  int l = first + (nlines > 0 ? (int)((unsigned)tile % (unsigned)nlines) : 0);
+  auto after = [&](int c) { return c + 1 == first + nlines ? first : c + 1; };
+  // Line c asks for the rows of line c + S - 1, whose stage all waves have left, and
+  // for the wave's own entries of line c + S, whose place is free as soon as the wave
+  // has read line c's.  In this order they are on their way before line 0 too.
+  int next_h = l, next_w = l;
 #pragma unroll
-  for (int c = 0; c < S - 1; ++c)
+  for (int c = 0; c < S; ++c) {
     if (c < nlines) {
 #pragma unroll
-      for (int j = 0; j < kOps; ++j) issue_op(j, c, next);
-      next = next + 1 == nlines ? 0 : next + 1;
+      for (int j = kRowOps; j < kOps; ++j) issue_op(j, c, next_w);
+      next_w = after(next_w);
     }
-  int s = 0;
+    if (c < S - 1 && c < nlines) {
+#pragma unroll
+      for (int j = 0; j < kRowOps; ++j) issue_op(j, c, next_h);
+      next_h = after(next_h);
+    }
+  }
+  int s = 0, left = nlines;
   // One line: the products of its 128 columns, from zero, times both scales.
-  // FILL: the line that takes the place of the last one's is asked for bit by
-  // bit meanwhile: a CU keeps about 100 lines in flight, and a wave that asks
+  // FILL: it asks for rows and entries (2), for rows (1) or for nothing (0), bit by bit
+  // between the products: a CU keeps about 100 lines in flight, and a wave that asks
   // for more stands still.
   auto line = [&](auto fill) {
-    constexpr bool kFill = decltype(fill)::value;
-    if (kFill)
-      wait_vmcnt<(S - 2) * kOps>();  // this line is in once only the lines after it are in flight
+    constexpr int kFill = decltype(fill)::value;
+    // The line is in once only what was asked for after its rows is in flight.
+    if (kFill > 0)
+      wait_vmcnt<(S - 2) * kOps + 4>();
+    else if (left > 2 && S > 3)
+      wait_vmcnt<2 * kOps>();
+    else if (left > 1 && S > 2)
+      wait_vmcnt<kOps>();
     else
       wait_vmcnt<0>();
     lds_barrier();  // every wave's part is, and the last line has been read by all
@@ -174,6 +213,7 @@ void vocab_fp8_kernel(int M, int K, int V, int ntiles, int mtiles, const uint8_t
       wf[2 * j] = widen8(y[0], y[1], 1.f);
       wf[2 * j + 1] = widen8(y[2], y[3], 1.f);
     }
+    lds_wait();  // the entries' place is free
     // A group's sum is added, scaled, while the next group is multiplied.
     f32x16 sum[2];
     float f[2];
@@ -191,10 +231,14 @@ void vocab_fp8_kernel(int M, int K, int V, int ntiles, int mtiles, const uint8_t
             acc[mb - 1][0][e] = fmaf(sum[(mb - 1) & 1][e], f[(mb - 1) & 1], acc[mb - 1][0][e]);
         }
         sum[mb & 1] = mfma32x32x16(wf[2 * j + 1], h1, sum[mb & 1]);
-        if (kFill) {
+        if (kFill > 0) {
           const int i = 4 * mb + j;
 #pragma unroll
-          for (int o = i * kOps / kSteps; o < (i + 1) * kOps / kSteps; ++o) issue_op(o, sp, next);
+          for (int o = i * kOps / kSteps; o < (i + 1) * kOps / kSteps; ++o)
+            if (o < kRowOps)
+              issue_op(o, sp, next_h);
+            else if (kFill > 1)
+              issue_op(o, s, next_w);
         }
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -202,54 +246,89 @@ void vocab_fp8_kernel(int M, int K, int V, int ntiles, int mtiles, const uint8_t
 #pragma unroll
     for (int e = 0; e < 16; ++e)
       acc[MB - 1][0][e] = fmaf(sum[(MB - 1) & 1][e], f[(MB - 1) & 1], acc[MB - 1][0][e]);
-    if (kFill) next = next + 1 == nlines ? 0 : next + 1;
+    if (kFill > 0) next_h = after(next_h);
+    if (kFill > 1) next_w = after(next_w);
     s = s + 1 == S ? 0 : s + 1;
-    l = l + 1 == nlines ? 0 : l + 1;
+    l = after(l);
+    --left;
   };
   sw_all = wsc[min((l & ~63) + lane, nscales - 1)];
-  int c = 0;
-  for (; c + S - 1 < nlines; ++c) {
-    if ((l & 63) == 0) sw_all = wsc[min(l + lane, nscales - 1)];
-    line(Flag<true>());
+  auto scales = [&]() {
+    if ((l & 63) == 0 || l == first) sw_all = wsc[min((l & ~63) + lane, nscales - 1)];
+  };
+  while (left > S) {
+    scales();
+    line(Int<2>());
   }
-  for (; c < nlines; ++c) {
-    if ((l & 63) == 0) sw_all = wsc[min(l + lane, nscales - 1)];
-    line(Flag<false>());
+  if (left == S) {
+    scales();
+    line(Int<1>());
   }
-  if (nscales > nlines) {  // the columns past the last whole line: 32, 64 or 96
-    const int units = (K - nlines * kColBlock) / 16;
+  while (left > 0) {
+    scales();
+    line(Int<0>());
+  }
+  if (kParts > 1 && part == 0 && all_lines % kParts != 0) lds_barrier();  // the last part's odd line
+  if (nscales > all_lines) {  // the columns past the last whole line: 32, 64 or 96
+    const int units = (K - all_lines * kColBlock) / 16;
     lds_barrier();
+    if (part == kParts - 1) {
 #pragma unroll
-    for (int o = 0; o < kOps; ++o) issue_op(o, 0, nlines, units);
-    wait_vmcnt<0>();
+      for (int o = 0; o < kOps; ++o) issue_op(o, 0, all_lines, units);
+      wait_vmcnt<0>();
+    }
     lds_barrier();
-    const float sw = wsc[nlines];
-    for (int j = 0; j < units / 2; ++j) {
-      const unsigned char* p = at(0, j);
-      const u32x4 y = *reinterpret_cast<const u32x4*>(p + (kHBlocks + wave * 4) * 1024);
-      const bf16x8 w0 = widen8(y[0], y[1], 1.f), w1 = widen8(y[2], y[3], 1.f);
+    if (part == kParts - 1) {
+      const float sw = wsc[all_lines];
+      for (int j = 0; j < units / 2; ++j) {
+        const unsigned char* p = at(0, j);
+        const u32x4 y = *reinterpret_cast<const u32x4*>(p + (kHBlocks + wave * 4) * 1024);
+        const bf16x8 w0 = widen8(y[0], y[1], 1.f), w1 = widen8(y[2], y[3], 1.f);
 #pragma unroll
-      for (int mb = 0; mb < MB; ++mb) {
-        const u32x4 x = read(p, mb);
-        f32x16 sum = {};
-        sum = mfma32x32x16(w0, widen8(x[0], x[1], 1.f), sum);
-        sum = mfma32x32x16(w1, widen8(x[2], x[3], 1.f), sum);
-        const float f = reinterpret_cast<const float*>(lds + kScaleAt)[mb * 32 + r] * sw;
+        for (int mb = 0; mb < MB; ++mb) {
+          const u32x4 x = read(p, mb);
+          f32x16 sum = {};
+          sum = mfma32x32x16(w0, widen8(x[0], x[1], 1.f), sum);
+          sum = mfma32x32x16(w1, widen8(x[2], x[3], 1.f), sum);
+          const float f = reinterpret_cast<const float*>(lds + kScaleAt)[mb * 32 + r] * sw;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) acc[mb][0][e] = fmaf(sum[e], f, acc[mb][0][e]);
-        __builtin_amdgcn_sched_barrier(0);
+          for (int e = 0; e < 16; ++e) acc[mb][0][e] = fmaf(sum[e], f, acc[mb][0][e]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
     }
   }
   lds_barrier();
+  if (kParts > 1) {
+    f32x4* const sums = reinterpret_cast<f32x4*>(lds_all) + wave * (MB * 4 * kWave) + lane;
+    if (part == 1) {
+#pragma unroll
+      for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          sums[(mb * 4 + g) * kWave] =
+              f32x4{acc[mb][0][4 * g], acc[mb][0][4 * g + 1], acc[mb][0][4 * g + 2], acc[mb][0][4 * g + 3]};
+    }
+    lds_barrier();
+    if (part == 1) return;  // the barriers that follow count the waves that are left
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const f32x4 o = sums[(mb * 4 + g) * kWave];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[mb][0][4 * g + e] += o[e];
+      }
+    lds_barrier();
+  }
   tile_epilogue32<MB, 1, NW>(acc, M, V, ntiles, tile, m0, blk0, logits, partials,
-                             reinterpret_cast<float(*)[MB * 32]>(lds));
+                             reinterpret_cast<float(*)[MB * 32]>(lds_all));
 }
 
 template <int MB, int NW>
 hipError_t launch(const Fp8Plan& p, const void* hidden, const float* hidden_scale, const void* w, const float* w_scale,
                   float* logits, float2* partials, hipStream_t stream) {
-  hipLaunchKernelGGL((vocab_fp8_kernel<MB, NW>), dim3((p.ntiles + 7) / 8 * 8 * p.mtiles), dim3(NW * kWave), 0, stream,
+  hipLaunchKernelGGL((vocab_fp8_kernel<MB, NW>), dim3((p.ntiles + 7) / 8 * 8 * p.mtiles), dim3(kWaves * kWave), 0, stream,
                      p.M, p.K, p.V, p.ntiles, p.mtiles, static_cast<const uint8_t*>(hidden), hidden_scale,
                      static_cast<const uint8_t*>(w), w_scale, logits, partials);
   return hipGetLastError();
@@ -260,27 +339,29 @@ hipError_t launch(const Fp8Plan& p, const void* hidden, const float* hidden_scal
 Fp8Plan fp8_plan(int M, int K, int V) {
   Fp8Plan p{M, K, V, 0, 0, 0, 0};
   const int blocks = (M + 31) / 32;
-  p.mtiles = (blocks + 6) / 7;
+  const int most = (blocks + 4) / 5;  // tiles of at most 160 rows: two stages of two parts' lines fill LDS
+  p.nw = (int64_t)(V + 127) / 128 * most <= kCUs ? 4 : 8;
+  p.mtiles = p.nw == 4 ? most : (blocks + 6) / 7;
   p.mb = (blocks + p.mtiles - 1) / p.mtiles;
-  p.nw = M > 64 || V > 65536 ? 8 : 4;
   const int width = 32 * p.nw;
   p.ntiles = (V + width - 1) / width;
   return p;
 }
 
-size_t fp8_logits_bytes(const Fp8Plan& p) { return (size_t)p.M * p.ntiles * sizeof(float2); }
+// Of the narrow tiles, whichever are used: it grows with rows and entries.
+size_t fp8_logits_bytes(int M, int V) { return (size_t)M * ((V + 127) / 128) * sizeof(float2); }
 
 hipError_t launch_logits_fp8(const Fp8Plan& p, const void* hidden, const float* hidden_scale, const void* w,
                              const float* w_scale, float* logits, float* row_lse, void* ws, hipStream_t stream) {
   float2* partials = static_cast<float2*>(ws);
   hipError_t e = hipErrorInvalidValue;
-#define SDV_F(B)                                                                                             \
-  case B:                                                                                                    \
-    e = p.nw == 8 ? launch<B, 8>(p, hidden, hidden_scale, w, w_scale, logits, partials, stream)              \
-                  : launch<B, 4>(p, hidden, hidden_scale, w, w_scale, logits, partials, stream);             \
+#define SDV_F(B, N)                                                                               \
+  case 16 * B + N:                                                                                \
+    e = launch<B, N>(p, hidden, hidden_scale, w, w_scale, logits, partials, stream);              \
     break;
-  switch (p.mb) {
-    SDV_F(1) SDV_F(2) SDV_F(3) SDV_F(4) SDV_F(5) SDV_F(6) SDV_F(7)
+  switch (16 * p.mb + p.nw) {
+    SDV_F(1, 4) SDV_F(2, 4) SDV_F(3, 4) SDV_F(4, 4) SDV_F(5, 4)
+    SDV_F(1, 8) SDV_F(2, 8) SDV_F(3, 8) SDV_F(4, 8) SDV_F(5, 8) SDV_F(6, 8) SDV_F(7, 8)
     default: break;
   }
 #undef SDV_F

@@ -118,6 +118,8 @@ def check_logits(got, lse, a, sa, w, sw, what):
     (64, 544, 2000), (65, 128, 3000), (96, 2048, 777), (129, 320, 1500), (144, 8192, 700), (160, 8320, 300), (200, 512, 33000),
     (224, 1056, 40001), (225, 256, 2000), (320, 1024, 1700), (400, 64, 900), (7, 4096, 33001), (50, 128, 70003), (1, 16384, 40),
     (130, 256, 70000), (180, 128, 33001),
+    # Odd numbers of lines in two parts, more lines than a wave holds scales of, and the same with undivided columns.
+    (40, 20512, 700), (100, 17280, 900), (161, 384, 1200), (3, 64, 128), (97, 672, 33001), (192, 9120, 33000),
 ])
 def test_logits(M, K, V):
     rng = np.random.default_rng(M + K + V)
