@@ -3,9 +3,17 @@
 //   O = softmax(scale * Q K^T + mask) V,  K = code * 2^e of its 64-key block and head, V likewise.
 //
 // The G * group queries that share a KV head are the rows of one KV head.  One
-// wave per work item (chunk of whole 64-key blocks of one request, KV head,
-// group of rows), four independent items per workgroup; each item writes a
-// partial (maximum, sum, O) and the merge joins them in chunk order.
+// wave, a workgroup of its own, per work item (chunk of whole 64-key blocks of one
+// request, KV head, group of rows); each item writes a partial (maximum, sum, O)
+// and the merge joins them in chunk order.
+//
+// Bound by the cache's stream up to two 16-row blocks: 16 requests of 24,576 keys, 8 KV
+// heads, D = 128 (805 MB) take 128 us with one block, 6.3 TB/s, and 142 with two.  Each
+// block more adds about 25 us (185-193 with four, 210-215 with five), of which the vector
+// instructions of its 64 x 16 scores are the larger part and its matrix products
+// 12: registers allow one wave per SIMD there, and its phases follow one another.
+// Taking the next half's products beside a half's exponentials left four blocks
+// at 193 us and made five spill (237); DMAs spread evenly over all products, 205.
 //
 // The cache is laid out in the order in which the matrix instructions take
 // their operands (sdverify_fp8.h): a lane's 16 bytes of K are two 32-wide steps
@@ -572,7 +580,9 @@ int blocks_of(int rows) {
 }
 
 // Workgroups (one wave, one item each) that run at once: what LDS holds, and at
-// head dimension 64 the registers of up to three blocks.
+// head dimension 64 the registers of up to three blocks.  16 requests of 24,576 keys, 8
+// heads of 48 rows, D = 64: 103 us with eight places, 128 with four; of 80 rows 162 with
+// four, 170 with eight.
 int64_t places(int rows, int D) { return cu_count() * (D == 64 && blocks_of(rows) <= 3 ? 8 : 4); }
 
 }  // namespace
@@ -587,14 +597,19 @@ AttnShape kv8_shape(int G, int Hq, int Hkv, int D, float scale, const int32_t* k
   s.rows = G * s.group;
   s.row_groups = row_groups(s.rows);
   s.scale_log2 = scale * kLog2e;
-  // For one to four rounds of items over the CUs' places the shortest chunk that
-  // fits them; of these the one that is done first.  One round takes a chunk and
-  // an item's start (rows, pages, first block, partial, in keys); items in more
-  // rounds are handed out as places come free, and the last ones end half a
-  // chunk apart.  More items than four rounds only with the longest chunk: the
-  // workspace holds no more partials.
+  // For a half to four rounds of items over the CUs' places the shortest chunk that
+  // fits them; of these the one that is done first, counted in keys of a wave with up to
+  // three blocks (with more a wave's own instructions bound it).  Up to one round
+  // takes a chunk and an item's start (rows, pages, first block); items in more rounds
+  // are handed out as places come free, and the last ones end half a chunk apart.  Then
+  // the partials are written and read, 8 keys' bytes a row.  More items than
+  // four rounds only with the longest chunk: the workspace holds no more partials.
+  // 8,000 keys, 8 heads of 40 rows, D = 128: 25.6 us so, 37 without the half round and the
+  // partials' cost; 13 requests of 1,500 keys, 48 rows, D = 64: 21.3 and 24.2; with 80
+  // rows 28.5, and 30.5 where five blocks count as three.
   const int64_t slots = places(s.rows, D);
   const int64_t start = 192 + 2 * s.rows;
+  const int work = blocks_of(s.rows) > 3 ? 3 : 2;
   auto items = [&](int tiles) {
     const int keys = tiles * kKeyBlock;
     int64_t n = 0;
@@ -605,15 +620,18 @@ AttnShape kv8_shape(int G, int Hq, int Hkv, int D, float scale, const int32_t* k
   int64_t best = INT64_MAX;
   int most = kMaxTiles;
   s.chunk_keys = kMaxTiles * kKeyBlock;
-  for (int r = 1; r <= 4; ++r) {
-    if (items(most) > r * slots) continue;
+  for (int r : {1, 2, 4, 6, 8}) {  // half rounds
+    const int64_t fit = r * slots / 2;
+    if (items(most) > fit) continue;
     int lo = 1, hi = most;  // the shortest chunk lies in [lo, hi]
     while (lo < hi) {
       const int mid = (lo + hi) / 2;
-      if (items(mid) <= r * slots) hi = mid; else lo = mid + 1;
+      if (items(mid) <= fit) hi = mid; else lo = mid + 1;
     }
     const int64_t keys = int64_t(lo) * kKeyBlock;
-    const int64_t cost = r == 1 ? keys + start : (total + items(lo) * start) / slots + keys / 2;
+    const int64_t n = items(lo);
+    const int64_t cost = (r <= 2 ? keys * work / 2 + start : (total * work / 2 + n * start) / slots + keys / 2) +
+                         n * s.rows * 8 / slots;
     if (cost < best) {
       best = cost;
       s.chunk_keys = lo * kKeyBlock;
