@@ -36,6 +36,7 @@
 // its reference maximum, and later ones may exceed it by 2^64, far within
 // float32 and bfloat16.  A row that outgrows that makes the wave take the maxima
 // of all blocks from there on and start its item again, once.
+#include <algorithm>
 #include <atomic>
 
 #include "fp8.h"
@@ -643,9 +644,9 @@ AttnShape kv8_shape(int G, int Hq, int Hkv, int D, float scale, const int32_t* k
 }
 
 int64_t kv8_max_chunks(int rows, int Hkv, int D, int B, int64_t max_kv_len) {
-  const int64_t most = 4 * places(rows, D) / Hkv;
+  const int64_t most = std::min(4 * places(rows, D) / Hkv, B * ((max_kv_len + kKeyBlock - 1) / kKeyBlock));
   const int64_t at_longest = B * ((max_kv_len + kMaxTiles * kKeyBlock - 1) / (kMaxTiles * kKeyBlock));
-  return most > at_longest ? most : at_longest;
+  return std::max(most, at_longest);
 }
 
 hipError_t launch_kv8_attention(const AttnShape& s, const AttnBatch& batch, const Kv8Pool& pool, int nchunks,

@@ -51,6 +51,13 @@ def test_workspace_bytes():
     assert sd.sd_fp8_workspace_bytes(dims(flags=1), 1000) == 0
 
 
+@pytest.mark.parametrize("vocab", [100, 32000, 33000, 128256])
+def test_projection_workspace_grows_with_rows(vocab):
+    """A projection's workspace for a large batch serves every smaller one (heads none: the attention has no part)."""
+    n = [sd.sd_fp8_workspace_bytes(dims(batch=b, gamma=0, n_q_heads=0, vocab=vocab), 1) for b in range(1, 700)]
+    assert all(0 < a <= b for a, b in zip(n, n[1:]))
+
+
 CACHES = [dict(k=None), dict(v=None), dict(k_scale=None), dict(v_scale=None), dict(block_table=None), dict(k=P + 8),
           dict(v=P + 4), dict(block_table=P + 2), dict(page_size=32), dict(page_size=96), dict(page_size=8192),
           dict(max_pages=0), dict(num_pages=0)]
@@ -134,6 +141,7 @@ def test_norm_refuses(kw, ptr, status):
 @cpu_only
 @pytest.mark.parametrize("kw,ptr,status", [
     (dict(hidden=100), {}, UNSUPPORTED), (dict(vocab=0), {}, BAD), (dict(vocab=3_000_000), {}, UNSUPPORTED),
+    (dict(hidden=2 ** 23 + 32), {}, UNSUPPORTED), (dict(batch=2 ** 22 + 1), {}, UNSUPPORTED),
     (dict(gamma=-1), {}, BAD), (dict(flags=1), {}, BAD), (dict(batch=1 << 24, gamma=1), {}, UNSUPPORTED), ({}, dict(h=None), BAD),
     ({}, dict(h=P + 8), BAD), ({}, dict(hs=P + 2), BAD), ({}, dict(w=P + 4), BAD), ({}, dict(ws=None), BAD),
     ({}, dict(lo=P + 4), BAD), ({}, dict(lse=None), BAD), ({}, dict(work=None), BAD), ({}, dict(n=8), WORKSPACE),
