@@ -40,7 +40,8 @@ HIPCC_FLAGS = [
 EXTRA_FLAGS = {
     "attention.hip": ["-fno-honor-nans", "-mno-amdgpu-ieee"],
     # The same for 8-bit caches; their NaN codes are found with integer operations.
-    "kv8_attention.hip": ["-fno-honor-nans", "-mno-amdgpu-ieee"],
+    # Matrix products into vector registers, where the softmax needs the scores.
+    "kv8_attention.hip": ["-fno-honor-nans", "-mno-amdgpu-ieee", "-mllvm", "-amdgpu-mfma-vgpr-form=1"],
 }
 
 

@@ -40,7 +40,7 @@ hipError_t launch_kv8_append(const Kv8Append& a, const Kv8Pool& pool, int Hkv, i
 // count of any lengths up to max_kv_len.  AttnBatch is used without kv_off and
 // pages.
 AttnShape kv8_shape(int G, int Hq, int Hkv, int D, float scale, const int32_t* kv_len, int B);
-int64_t kv8_max_chunks(int rows, int Hkv, int D, int B, int64_t max_kv_len);
+int64_t kv8_max_chunks(int Hkv, int D, int B, int64_t max_kv_len);
 hipError_t launch_kv8_attention(const AttnShape& s, const AttnBatch& batch, const Kv8Pool& pool, int nchunks,
                                 const void* q, AttnPartials parts, void* out, hipStream_t stream);
 

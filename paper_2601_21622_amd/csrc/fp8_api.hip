@@ -93,7 +93,7 @@ size_t sd_fp8_workspace_bytes(const sd_dims_t* d, int32_t max_kv_len) {
   size_t n = 0;
   if (check_attention(d) == SD_OK && max_kv_len > d->gamma && max_kv_len <= kMaxKvLen) {
     const int rows = (d->gamma + 1) * (d->n_q_heads / d->n_kv_heads);
-    const int64_t chunks = kv8_max_chunks(rows, d->n_kv_heads, d->head_dim, d->batch, max_kv_len);
+    const int64_t chunks = kv8_max_chunks(d->n_kv_heads, d->head_dim, d->batch, max_kv_len);
     n = align_up(attn_partial_bytes(chunks, d->n_kv_heads, rows, d->head_dim));
   }
   if (check_projection(d) == SD_OK)

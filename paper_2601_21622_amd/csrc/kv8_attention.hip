@@ -8,12 +8,12 @@
 // and the merge joins them in chunk order.
 //
 // Bound by the cache's stream up to two 16-row blocks: 16 requests of 24,576 keys, 8 KV
-// heads, D = 128 (805 MB) take 128 us with one block, 6.3 TB/s, and 142 with two.  Each
-// block more adds about 25 us (185-193 with four, 210-215 with five), of which the vector
+// heads, D = 128 (805 MB) take 128-133 us with one block, 6.1-6.3 TB/s, and 145 with
+// two.  Each block more adds about 21 us (187 with four, 206 with five), of which the vector
 // instructions of its 64 x 16 scores are the larger part and its matrix products
-// 12: registers allow one wave per SIMD there, and its phases follow one another.
-// Taking the next half's products beside a half's exponentials left four blocks
-// at 193 us and made five spill (237); DMAs spread evenly over all products, 205.
+// 12: LDS and registers allow one wave per SIMD there, and its phases follow one another.
+// Scores are kept in vector registers by the build's choice of instruction form: in
+// accumulation registers every score is moved once more (four blocks 194 us, five 214).
 //
 // The cache is laid out in the order in which the matrix instructions take
 // their operands (sdverify_fp8.h): a lane's 16 bytes of K are two 32-wide steps
@@ -343,8 +343,11 @@ __device__ __forceinline__ void spread_nan(Wave8<RB, D>& w, const unsigned char*
   }
 }
 
+// At head dimension 64 LDS holds two waves per SIMD, and half the registers each are
+// enough (five blocks spill 36): 16 requests of 24,576 keys, 8 heads: of 64 rows 105 us,
+// 133 with one wave per SIMD; of 72 rows 118 and 149.
 template <int RB, int D>
-__global__ __launch_bounds__(kWave, 1)
+__global__ __launch_bounds__(kWave, D == 64 ? 2 : 1)
 void kv8_attn_kernel(AttnShape s, AttnBatch bt, Kv8Pool pool, int nchunks, const uint16_t* __restrict__ q,
                      AttnPartials parts) {
   using R = Ring<D>;
@@ -606,11 +609,8 @@ int blocks_of(int rows) {
   return ((rows + 15) / 16 + g - 1) / g;
 }
 
-// Workgroups (one wave, one item each) that run at once: what LDS holds, and at
-// head dimension 64 the registers of up to three blocks.  16 requests of 24,576 keys, 8
-// heads of 48 rows, D = 64: 103 us with eight places, 128 with four; of 80 rows 162 with
-// four, 170 with eight.
-int64_t places(int rows, int D) { return cu_count() * (D == 64 && blocks_of(rows) <= 3 ? 8 : 4); }
+// Workgroups (one wave, one item each) that run at once: what LDS holds.
+int64_t places(int D) { return cu_count() * (D == 64 ? 8 : 4); }
 
 }  // namespace
 
@@ -631,10 +631,10 @@ AttnShape kv8_shape(int G, int Hq, int Hkv, int D, float scale, const int32_t* k
   // are handed out as places come free, and the last ones end half a chunk apart.  Then
   // the partials are written and read, 8 keys' bytes a row.  More items than
   // four rounds only with the longest chunk: the workspace holds no more partials.
-  // 8,000 keys, 8 heads of 40 rows, D = 128: 25.6 us so, 37 without the half round and the
-  // partials' cost; 13 requests of 1,500 keys, 48 rows, D = 64: 21.3 and 24.2; with 80
-  // rows 28.5, and 30.5 where five blocks count as three.
-  const int64_t slots = places(s.rows, D);
+  // Before and after the half round and the partials' cost came in: 8,000 keys, 8
+  // heads of 40 rows, D = 128, 37 and 25.6 us; 13 requests of 1,500 keys, 48 rows, D = 64,
+  // 24.2 and 21.3; with 80 rows, D = 128, 41.7 where five blocks count as three, 37.6 as it is.
+  const int64_t slots = places(D);
   const int64_t start = 192 + 2 * s.rows;
   const int work = blocks_of(s.rows) > 3 ? 3 : 2;
   auto items = [&](int tiles) {
@@ -669,8 +669,8 @@ AttnShape kv8_shape(int G, int Hq, int Hkv, int D, float scale, const int32_t* k
   return s;
 }
 
-int64_t kv8_max_chunks(int rows, int Hkv, int D, int B, int64_t max_kv_len) {
-  const int64_t most = std::min(4 * places(rows, D) / Hkv, B * ((max_kv_len + kKeyBlock - 1) / kKeyBlock));
+int64_t kv8_max_chunks(int Hkv, int D, int B, int64_t max_kv_len) {
+  const int64_t most = std::min(4 * places(D) / Hkv, B * ((max_kv_len + kKeyBlock - 1) / kKeyBlock));
   const int64_t at_longest = B * ((max_kv_len + kMaxTiles * kKeyBlock - 1) / (kMaxTiles * kKeyBlock));
   return std::max(most, at_longest);
 }
