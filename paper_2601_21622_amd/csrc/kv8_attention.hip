@@ -394,12 +394,13 @@ void kv8_attn_kernel(AttnShape s, AttnBatch bt, Kv8Pool pool, int nchunks, const
     for (int j = i; j < n; ++j) ring_dma(src + j * 1024, off, dst + j * 1024);
   };
   const int halves = __builtin_amdgcn_readfirstlane(2 * ntiles);
-  // Half n is in: of those after it, as many as are on their way may still be.
-  auto wait_half = [&](int n) {
-    static_assert((R::kSlots - 2) * R::kOps < 64, "vmcnt holds 6 bits");
+  // Half n is in once only DMAs of later halves are on their way: of as many as were
+  // asked for by then, MOST if there are that many.
+  auto wait_half = [&](int n, auto most) {
+    constexpr int kMost = decltype(most)::value;
+    static_assert(kMost > 2 * R::kOps && kMost <= 3 * R::kOps && kMost < 64, "vmcnt holds 6 bits");
     const int after = halves - 1 - n;
-    if (after >= R::kSlots - 2) wait_vmcnt<(R::kSlots - 2) * R::kOps>();
-    else if (after >= 3) wait_vmcnt<3 * R::kOps>();
+    if (after >= 3) wait_vmcnt<kMost>();
     else if (after == 2) wait_vmcnt<2 * R::kOps>();
     else if (after == 1) wait_vmcnt<R::kOps>();
     else wait_vmcnt<0>();
@@ -473,10 +474,13 @@ void kv8_attn_kernel(AttnShape s, AttnBatch bt, Kv8Pool pool, int nchunks, const
       const int vs = ks + 1 == R::kSlots ? 0 : ks + 1;    // place of V of block t
       const int last = ks == 0 ? R::kSlots - 1 : ks - 1;  // of V of block t - 1, free now
       const int nv = 2 * t - 1 + R::kSlots, nk = nv + 1;  // the halves that take free places
-      wait_half(2 * t);
+      // Before K of block t is read, three halves after it have been asked for; before V,
+      // two and half of the one that takes the last V's place.
+      static_assert(R::kSlots == 5, "as many as the waits count");
+      wait_half(2 * t, Int<3 * R::kOps>());
       done = fold_block<RB, D, MASKED>(
           w, ring + ks * R::kHalf + off, ring + vs * R::kHalf + off, pow2(ks_all, t), pow2(vs_all, t), s.scale_log2,
-          key_begin + t * kKeyBlock, first, end, [&] { wait_half(2 * t + 1); },
+          key_begin + t * kKeyBlock, first, end, [&] { wait_half(2 * t + 1, Int<5 * R::kOps / 2>()); },
           [&](int n) {
             if (t > 0 && nv < halves) fetch(nv, last, n * R::kOps / 4, (n + 1) * R::kOps / 4);
           },
