@@ -605,13 +605,20 @@ int64_t cu_count() {
   return n;
 }
 
-// One wave holds up to five 16-row blocks (at head dimension 128 O takes 32
-// registers of each, Q 16); more rows are split over row groups, a wave each.
-int row_groups(int rows) { return (rows + 16 * kMaxBlocks - 1) / (16 * kMaxBlocks); }
-int blocks_of(int rows) {
-  const int g = row_groups(rows);
-  return ((rows + 15) / 16 + g - 1) / g;
+// 16-row blocks of a wave.  One holds up to five (at head dimension 128 O takes 32
+// registers of each, Q 16); more rows are split over row groups, a wave each.  Where the
+// caches are a few blocks of keys per place, what counts is how long a wave takes for
+// its own: two row blocks, or one where three would leave a wave half empty, and
+// the groups read the same keys from L2.  `blocks`: 64-key blocks times heads.
+// 64 rows, D = 128, 8 heads: 4 requests of 1,500 keys (768 blocks) 17.9 us so and 22.0
+// with four row blocks, 16 of 3,000 (6,016) 43.9 and 45.6, 64 of 2,000 (16,384) 87.7 and
+// 77.1; 48 rows, D = 64, 13 of 1,500 (2,496) 18.7 with one, 20.9 with two, 19.9 with three.
+int row_groups(int rows, int64_t blocks) {
+  const int b = (rows + 15) / 16;
+  const int most = blocks > 32 * cu_count() ? kMaxBlocks : b == 3 ? 1 : 2;
+  return (b + most - 1) / most;
 }
+int blocks_of(int rows, int groups) { return ((rows + 15) / 16 + groups - 1) / groups; }
 
 // Workgroups (one wave, one item each) that run at once: what LDS holds.
 int64_t places(int D) { return cu_count() * (D == 64 ? 8 : 4); }
@@ -626,7 +633,9 @@ AttnShape kv8_shape(int G, int Hq, int Hkv, int D, float scale, const int32_t* k
   s.D = D;
   s.group = Hq / Hkv;
   s.rows = G * s.group;
-  s.row_groups = row_groups(s.rows);
+  int64_t blocks = 0;
+  for (int b = 0; b < B; ++b) blocks += (kv_len[b] + kKeyBlock - 1) / kKeyBlock;
+  s.row_groups = row_groups(s.rows, blocks * Hkv);
   s.scale_log2 = scale * kLog2e;
   // For a half to four rounds of items over the CUs' places the shortest chunk that
   // fits them; of these the one that is done first, counted in keys of a wave with up to
@@ -640,7 +649,7 @@ AttnShape kv8_shape(int G, int Hq, int Hkv, int D, float scale, const int32_t* k
   // 24.2 and 21.3; with 80 rows, D = 128, 41.7 where five blocks count as three, 37.6 as it is.
   const int64_t slots = places(D);
   const int64_t start = 192 + 2 * s.rows;
-  const int work = blocks_of(s.rows) > 3 ? 3 : 2;
+  const int work = blocks_of(s.rows, s.row_groups) > 3 ? 3 : 2;
   auto items = [&](int tiles) {
     const int keys = tiles * kKeyBlock;
     int64_t n = 0;
@@ -691,7 +700,7 @@ hipError_t launch_kv8_attention(const AttnShape& s, const AttnBatch& batch, cons
       hipLaunchKernelGGL((kv8_attn_kernel<RB, 64>), grid, block, 0, stream, s, batch, pool, nchunks,               \
                          static_cast<const uint16_t*>(q), parts);                                                 \
     break;
-  switch (blocks_of(s.rows)) {
+  switch (blocks_of(s.rows, s.row_groups)) {
     SDV_KV8(1) SDV_KV8(2) SDV_KV8(3) SDV_KV8(4) SDV_KV8(5)
     default: return hipErrorInvalidValue;
   }

@@ -249,6 +249,56 @@ def test_attention_of_long_chunks(G, Hq, Hkv, D, page, tree):
     announce(f"kv8 attention of long chunks G {G} D {D}: {worst:.2f} of the bound")
 
 
+@pytest.mark.parametrize("G,D", [(5, 64), (8, 64), (9, 64), (16, 64), (5, 128), (8, 128), (9, 128), (16, 128)])
+def test_attention_of_many_blocks(G, D):
+    """Past 8,192 blocks of keys a wave holds all rows of a head that it can: 40, 64, 72 and 128 rows."""
+    rng = np.random.default_rng(10 * G + D)
+    Hkv, lens = 32, [3400, 3333, 3329, 3328, 3210]
+    c = Cache(rng, lens, Hkv, D, 256)
+    for a in (c.k, c.v):  # numbers up to 1 (code 0x38) and their negatives
+        a[...] = rng.integers(0, 0x39, a.shape, dtype=np.uint8) | rng.integers(0, 2, a.shape, dtype=np.uint8) << 7
+    c.ks[...] = 127 + rng.integers(-1, 2, c.ks.shape)
+    c.vs[...] = 127 + rng.integers(-1, 2, c.vs.shape)
+    c.upload()
+    q = torch.from_numpy(rng.normal(size=(len(lens), G, 8 * Hkv, D)) * 2).bfloat16()
+    got = attend(G, 8 * Hkv, Hkv, D, c, lens, q.cuda(), None, 1 / np.sqrt(D))
+    for b in (0, 2, 4):  # each request against the oracle by itself
+        seg = fp8.kv8_segments(c.k, c.v, c.ks, c.vs, c.table[b:b + 1], lens[b:b + 1])
+        check_attention(got[b:b + 1], q[b:b + 1].double().numpy(), seg, lens[b:b + 1], Hkv, None, 1 / np.sqrt(D),
+                        f"many blocks, request {b}")
+
+
+@pytest.mark.parametrize("G,D", [(5, 64), (9, 64), (5, 128), (8, 128), (9, 128)])
+def test_jumps_and_nan_among_many_blocks(G, D):
+    """As test_attention_of_scores_that_jump (one product makes a score: exact but for the
+    factors, 3 * 2^-24 * 256 of p), with three to five row blocks to a wave; and one NaN value that positions
+    2 .. of one head see."""
+    rng = np.random.default_rng(20 * G + D)
+    Hkv, lens, page = 32, [3400, 3333, 3329, 3328, 3210], 256
+    c = Cache(rng, lens, Hkv, D, page)
+    c.k[...] = 0
+    c.k[..., fp8.k_index(D)[:, 0]] = rng.integers(0x28, 0x39, (*c.k.shape[:3], 64))  # 1/4 .. 1
+    c.v[...] = rng.integers(0, 0x39, c.v.shape, dtype=np.uint8) | rng.integers(0, 2, c.v.shape, dtype=np.uint8) << 7
+    c.ks[...] = 127 + rng.choice([0, 0, 5, 7, 8], c.ks.shape)
+    c.vs[...] = 127
+    clean = c.v.copy()
+    key, head, col = lens[0] - G + 2, 3, 7
+    c.v[c.table[0, key // page], head, key % page // 64, fp8.v_index(D)[key % 64, col]] = 0x7f
+    c.upload()
+    q = torch.zeros((len(lens), G, 8 * Hkv, D), dtype=torch.bfloat16)
+    q[..., 0] = torch.from_numpy(rng.choice([1.0, -1.0, 0.5], q.shape[:3])).bfloat16()
+    got = attend(G, 8 * Hkv, Hkv, D, c, lens, q.cuda(), None, 1.0)
+    hit = got[0, 2:, 8 * head:8 * head + 8, col]
+    assert np.isnan(hit).all() and np.isnan(got).sum() == hit.size
+    for b in (0, 3):
+        seg = fp8.kv8_segments(c.k, clean, c.ks, c.vs, c.table[b:b + 1], lens[b:b + 1])
+        if b == 0:  # the spoilt outputs: as the oracle's
+            ref = verify_attention(q[:1].double().numpy(), *seg, lens[:1], Hkv, 1.0)
+            got[0, 2:, 8 * head:8 * head + 8, col] = ref[0, 2:, 8 * head:8 * head + 8, col]
+        check_attention(got[b:b + 1], q[b:b + 1].double().numpy(), seg, lens[b:b + 1], Hkv, None, 1.0,
+                        f"jumps among many blocks, request {b}")
+
+
 @pytest.mark.parametrize("G,Hq,Hkv,D", [(2, 16, 16, 128), (5, 16, 16, 64), (10, 32, 4, 128)])
 def test_attention_of_scores_that_jump(G, Hq, Hkv, D):
     """Scores rise and fall by hundreds from one stretch of keys to the next, inside
