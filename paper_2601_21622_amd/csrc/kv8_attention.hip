@@ -415,7 +415,7 @@ void kv8_attn_kernel(AttnShape s, AttnBatch bt, Kv8Pool pool, int nchunks, const
 
   Wave8<RB, D> w;
   const int whole = min(max((first + 1 - key_begin) / kKeyBlock, 0), ntiles);  // blocks that every row sees whole
-  uint64_t masks = 0;
+  uint64_t masks = 1;  // a chunk of whole blocks ends with position 0 at the latest: all rows see it
   if (whole < ntiles) masks = position_mask(bt.parent != nullptr ? bt.parent + (int64_t)req * (s.G - 1) : nullptr, s.G);
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {

@@ -483,3 +483,35 @@ def test_binding_refuses_what_does_not_fit():
             bad()
     with pytest.raises(sd.SdError):
         sd.sd_verify_attention_kv8(d, q, c.handle, [65], None, 1.0, torch.empty_like(q), ws)
+
+
+# Chunks that end with the key of position 0: no block of them is masked, and its last key
+# is the step's own.  (G, lengths, heads) with chunks of one block, and of several.
+ENDS = {
+    "one_token": (1, [64, 128, 1024], 2),
+    "one_token_long_chunks": (1, [1408 - 64 * (i % 5) for i in range(24)], 16),
+    "five_tokens": (5, [68, 132, 708], 2),
+    "five_tokens_long_chunks": (5, [1412 - 64 * (i % 5) for i in range(24)], 16),
+}
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("name", ENDS)
+def test_attention_of_a_far_score_at_the_end_of_whole_blocks(name, D):
+    """The key of position 0 scores 300 above all others and ends a block: the largest
+    score of its chunk is found.  One column alone makes a score, as in test_attention_of_scores_that_jump."""
+    G, lens, H = ENDS[name]
+    rng = np.random.default_rng(G + D)
+    off = np.cumsum([0] + lens[:-1])
+    x = [rng.normal(size=(sum(lens), H, D)) for _ in range(2)]
+    x[0][...] = 0.0
+    x[0][..., 0] = rng.normal(size=(sum(lens), H))
+    x[0][off + np.array(lens) - G, :, 0] = 300.0
+    c = Cache(rng, lens, H, D, 64)
+    c.append(*x, off, lens, lens)
+    c.upload()
+    q = torch.zeros((len(lens), G, H, D), dtype=torch.bfloat16)
+    q[..., 0] = 1.0
+    got = attend(G, H, H, D, c, lens, q.cuda(), None, 1.0)
+    seg = fp8.kv8_segments(c.k, c.v, c.ks, c.vs, c.table, lens)
+    check_attention(got, q.double().numpy(), seg, lens, H, None, 1.0, name)
