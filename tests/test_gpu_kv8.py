@@ -515,3 +515,79 @@ def test_attention_of_a_far_score_at_the_end_of_whole_blocks(name, D):
     got = attend(G, H, H, D, c, lens, q.cuda(), None, 1.0)
     seg = fp8.kv8_segments(c.k, c.v, c.ks, c.vs, c.table, lens)
     check_attention(got, q.double().numpy(), seg, lens, H, None, 1.0, name)
+
+
+def put_rows(c, pool, index, b, codes):
+    """Codes [L][heads][D] of request b's keys into a pool of the cache's."""
+    for n0 in range(0, len(codes), 64):
+        part = codes[n0:n0 + 64].transpose(1, 0, 2)
+        block = pool[c.table[b, n0 // c.page], :, n0 % c.page // 64]
+        block[:, index[:part.shape[1]]] = part
+
+
+@pytest.mark.parametrize("G,Hq,Hkv,D,lens", [
+    (3, 8, 2, 128, [200, 333]), (3, 8, 2, 64, [200, 333]),
+    (5, 16, 16, 128, [1400 - 31 * i for i in range(24)]), (5, 16, 16, 64, [1400 - 31 * i for i in range(24)]),
+    (4, 32, 4, 128, [1400 - 31 * i for i in range(24)]),
+    (9, 256, 32, 128, [3400, 3333, 3329, 3328, 3210]), (9, 256, 32, 64, [3400, 3333, 3329, 3328, 3210])])
+def test_attention_of_huge_dense_queries(G, Hq, Hkv, D, lens):
+    """Queries of all columns up to 2^101: a score summed from zero and one summed from the
+    reference differ by their rounding, far more than the exponential takes.  Each row has one key of twice its signs, whose
+    score exceeds all others by thousands in the exponential: the output is that key's value, to the bit
+    (weights one and zero, a value of four bits)."""
+    rng = np.random.default_rng(G + D)
+    group = Hq // Hkv
+    c = Cache(rng, lens, Hkv, D, 64)
+    c.ks[...] = 127
+    c.vs[...] = 127
+    ki, vi = fp8.k_index(D), fp8.v_index(D)
+    q = rng.uniform(1, 2, (len(lens), G, Hq, D)) * rng.choice([-1.0, 1.0], (len(lens), G, Hq, D))
+    q = torch.from_numpy(q * 2.0 ** rng.choice([10, 20, 27, 28, 30, 40, 60, 100], (len(lens), G, Hq, 1))).bfloat16()
+    want = np.empty(q.shape)
+    for b, L in enumerate(lens):
+        k = (rng.integers(0x38, 0x40, (L, Hkv, D)) | rng.integers(0, 2, (L, Hkv, D)) << 7).astype(np.uint8)  # 1 .. 1.875
+        v = (rng.integers(0x20, 0x48, (L, Hkv, D)) | rng.integers(0, 2, (L, Hkv, D)) << 7).astype(np.uint8)
+        rows_of_head = q[b].double().numpy().reshape(G, Hkv, group, D).transpose(1, 0, 2, 3).reshape(Hkv, G * group, D)
+        for h in range(Hkv):
+            at = rng.permutation(L - G)[:G * group]
+            k[at, h] = 0x40 | np.where(rows_of_head[h] < 0, 0x80, 0)  # 2, the row's signs
+            want[b, :, h * group:(h + 1) * group] = fp8.decode(v[at, h]).reshape(G, group, D)
+            if h == 0:
+                s = rows_of_head[h] @ fp8.decode(k[:, h]).T
+                best = s[np.arange(len(at)), at].copy()
+                s[np.arange(len(at)), at] = -np.inf
+                assert ((best - s.max(axis=1)) / np.sqrt(D) > 2000).all()
+        put_rows(c, c.k, ki, b, k)
+        put_rows(c, c.v, vi, b, v)
+    c.upload()
+    got = attend(G, Hq, Hkv, D, c, lens, q.cuda(), None, 1 / np.sqrt(D))
+    assert np.array_equal(got, want), f"{(got != want).any(axis=3).sum()} rows differ"
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_nan_among_keys_that_are_taken_again(D):
+    """A far score late in each chunk takes the item up again; a NaN value early in one makes its column
+    NaN in its head, and nothing else."""
+    G, H = 3, 16
+    rng = np.random.default_rng(D)
+    lens = [1400 - 31 * i for i in range(24)]
+    off = np.cumsum([0] + lens[:-1])
+    x = [rng.normal(size=(sum(lens), H, D)) for _ in range(2)]
+    x[0][...] = 0.0
+    x[0][..., 0] = rng.normal(size=(sum(lens), H))
+    for o, n in zip(off, lens):
+        x[0][o + 50:o + n:64, :, 0] = 300.0 + np.arange(len(range(50, n, 64)))[:, None]
+    c = Cache(rng, lens, H, D, 64)
+    c.append(*x, off, lens, lens)
+    clean = c.v.copy()
+    c.v[c.table[2, 1], 1, 0, fp8.v_index(D)[3, 5]] = 0xff
+    c.upload()
+    q = torch.zeros((len(lens), G, H, D), dtype=torch.bfloat16)
+    q[..., 0] = 1.0
+    got = attend(G, H, H, D, c, lens, q.cuda(), None, 1.0)
+    seg = fp8.kv8_segments(c.k, clean, c.ks, c.vs, c.table, lens)
+    hit = np.zeros(got.shape, dtype=bool)
+    hit[2, :, 1, 5] = True
+    assert np.array_equal(np.isnan(got), hit)
+    got[hit] = verify_attention(q.double().numpy(), *seg, lens, H, 1.0)[hit]
+    check_attention(got, q.double().numpy(), seg, lens, H, None, 1.0, "taken again")
