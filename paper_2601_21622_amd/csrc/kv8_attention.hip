@@ -53,6 +53,7 @@ namespace {
 
 constexpr int kMaxBlocks = 5;   // 16-row blocks of a wave
 constexpr int kMaxTiles = 64;   // blocks per chunk: one lane holds one block's page
+constexpr float kNoKey = -3.402823466e38f;  // reference maximum of a row that has seen no key: no score lies below it
 constexpr float kGrowLog2 = 64.f;  // growth of a row's maximum that takes the item up anew
 
 // A wave's ring: halves of 64 D bytes, D / 16 DMAs of 1 KB each.  Four (D = 128) or
@@ -142,7 +143,7 @@ template <int RB, int D>
 struct Wave8 {
   bf16x8 q[RB][D / 32];
   f32x4 o[RB][D / 16];
-  float m[RB], l[RB];  // reference maximum of the unscaled scores (kNegBig: no key seen yet), sum
+  float m[RB], l[RB];  // reference maximum of the unscaled scores (kNoKey: no key seen yet), sum
   uint64_t sees[RB];   // of the step's own positions
   uint32_t nan;        // a NaN code was left out of O
 };
@@ -244,7 +245,7 @@ __device__ __forceinline__ bool fold_block(Wave8<RB, D>& w, const unsigned char*
     f32x4 sc[RB][2];
     float base[RB], mx[RB];
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) base[rb] = w.m[rb] > kNegBig && !known ? -w.m[rb] : 0.f;
+    for (int rb = 0; rb < RB; ++rb) base[rb] = w.m[rb] > kNoKey && !known ? -w.m[rb] : 0.f;
     half_scores<RB, D, MASKED>(w, k, hf, ks, key0 + 4 * lg - first, base, sc, refill_v);
     if (hf == 0) {
       read_k<D>(kp, 1, k);
@@ -257,16 +258,16 @@ __device__ __forceinline__ bool fold_block(Wave8<RB, D>& w, const unsigned char*
     bool grow = false, fresh = false;
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-      grow |= w.m[rb] > kNegBig && mx[rb] * scale_log2 > kGrowLog2;
-      fresh |= !(w.m[rb] > kNegBig) && mx[rb] > kNegBig;
+      grow |= w.m[rb] > kNoKey && mx[rb] * scale_log2 > kGrowLog2;
+      fresh |= !(w.m[rb] > kNoKey) && mx[rb] > kNoKey;
     }
     if (__builtin_expect(__ballot(grow) != 0, 0) && !known) return false;
     if (__builtin_expect(__ballot(fresh) != 0 || known, 0)) {  // rows' first keys: their maximum is the reference
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
-        const bool set = !known && !(w.m[rb] > kNegBig) && mx[rb] > kNegBig;
+        const bool set = !known && !(w.m[rb] > kNoKey) && mx[rb] > kNoKey;
         w.m[rb] = set ? mx[rb] : w.m[rb];
-        const float less = set || (known && w.m[rb] > kNegBig) ? w.m[rb] : 0.f;
+        const float less = set || (known && w.m[rb] > kNoKey) ? w.m[rb] : 0.f;
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -437,7 +438,7 @@ void kv8_attn_kernel(AttnShape s, AttnBatch bt, Kv8Pool pool, int nchunks, const
     for (int i = 0; i < D / 32; ++i) w.q[rb][i] = load_bf16x8(src + 64 * (i >> 1) + 8 * (i & 1));
     const uint32_t a = __shfl((uint32_t)masks, j), b = __shfl((uint32_t)(masks >> 32), j);
     w.sees[rb] = ((uint64_t)b << 32) | a;
-    w.m[rb] = kNegBig;
+    w.m[rb] = kNoKey;
   }
 
   auto pow2 = [&](int bytes, int t) {
@@ -548,7 +549,7 @@ void kv8_merge_kernel(AttnShape s, AttnBatch bt, AttnPartials parts, uint16_t* _
   const int head = blockIdx.y, b = blockIdx.z;
   const int row = i / (D / 4), d = i % (D / 4) * 4;
   const int c0 = bt.chunk_base + bt.chunk_prefix[b], c1 = bt.chunk_base + bt.chunk_prefix[b + 1];
-  float m = kNegBig, den = 0.f;
+  float m = kNoKey, den = 0.f;
   f32x4 num = {0.f, 0.f, 0.f, 0.f};
   // Chunks c .. c + N - 1, whose partials are on their way together.
   auto join = [&](int c, auto count) {

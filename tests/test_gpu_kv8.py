@@ -591,3 +591,27 @@ def test_nan_among_keys_that_are_taken_again(D):
     assert np.array_equal(np.isnan(got), hit)
     got[hit] = verify_attention(q.double().numpy(), *seg, lens, H, 1.0)[hit]
     check_attention(got, q.double().numpy(), seg, lens, H, None, 1.0, "taken again")
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_attention_of_scores_far_below_zero(D):
+    """Rows whose every score lies between -2^119 and -2^112: the key of the least magnitude has all the weight."""
+    rng = np.random.default_rng(D)
+    G, H, lens = 3, 2, [3, 64, 500, 1411]
+    c = Cache(rng, lens, H, D, 64)
+    c.ks[...] = 127
+    c.vs[...] = 127
+    q = torch.from_numpy(rng.uniform(1, 2, (len(lens), G, H, D)) * 2.0 ** 110).bfloat16()
+    want = np.empty(q.shape)
+    for b, L in enumerate(lens):
+        k = rng.integers(0xb8, 0xc0, (L, H, D)).astype(np.uint8)  # -1 .. -1.875
+        v = (rng.integers(0x20, 0x48, (L, H, D)) | rng.integers(0, 2, (L, H, D)) << 7).astype(np.uint8)
+        for h in range(H):
+            at = rng.integers(0, L - G + 1)
+            k[at, h] = 0xa8  # -1/4
+            want[b, :, h] = fp8.decode(v[at, h])
+        put_rows(c, c.k, fp8.k_index(D), b, k)
+        put_rows(c, c.v, fp8.v_index(D), b, v)
+    c.upload()
+    got = attend(G, H, H, D, c, lens, q.cuda(), None, 1 / np.sqrt(D))
+    assert np.array_equal(got, want)
