@@ -109,6 +109,8 @@ SD_API int sd_kv8_append(const sd_dims_t* dims, const sd_kv8_cache_t* cache, con
  *   scale    softmax scale, finite and > 0
  * G * (n_q_heads / n_kv_heads) <= 128.  Keys that a position does not see
  * contribute nothing, whatever they hold; a NaN that it sees makes its output NaN.
+ * Scores, and the sum of |V| over a request's keys, have to lie within float32's
+ * range: what passes it comes out as an infinity or NaN.
  */
 SD_API int sd_verify_attention_kv8(const sd_dims_t* dims, const void* q, const sd_kv8_cache_t* cache,
                                    const int32_t* kv_len, const int32_t* parent, float scale, void* out,

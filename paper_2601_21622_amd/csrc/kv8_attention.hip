@@ -33,8 +33,9 @@
 //
 // Softmax in the log2 domain.  O is never rescaled (a branch that does so made
 // the compiler spill up to 535 registers): a row's first scores in the chunk set
-// its reference maximum, and later ones may exceed it by 2^64, far within
-// float32 and bfloat16.  A row that outgrows that makes the wave take the maxima
+// its reference maximum, and later ones may exceed it by 2^64, less where V is so
+// large that the sum of so many weights times values could leave float32
+// (grow_limit).  A row that outgrows that makes the wave take the maxima
 // of all its blocks and start its item again, once: this time scores are summed
 // from zero, as they were for the maxima, and the reference is subtracted from the
 // sum.  That gives the same bits, so that no difference is above zero and the largest
@@ -54,7 +55,12 @@ namespace {
 constexpr int kMaxBlocks = 5;   // 16-row blocks of a wave
 constexpr int kMaxTiles = 64;   // blocks per chunk: one lane holds one block's page
 constexpr float kNoKey = -3.402823466e38f;  // reference maximum of a row that has seen no key: no score lies below it
-constexpr float kGrowLog2 = 64.f;  // growth of a row's maximum that takes the item up anew
+constexpr int kGrowLog2 = 64;   // growth of a row's maximum, log2, that takes the item up anew
+
+// The growth that weights of a block may have whose V scale byte is this: 2^30 keys
+// (the longest cache) of weight 2^limit and value 448 * 2^(byte - 127) sum to less than
+// 2^128.  None from byte 216 on, where the values alone have to sum to less.
+__device__ __forceinline__ float grow_limit(int v_byte) { return (float)min(max(216 - v_byte, 0), kGrowLog2); }
 
 // A wave's ring: halves of 64 D bytes, D / 16 DMAs of 1 KB each.  Four (D = 128) or
 // eight fill a CU's 160 KB.
@@ -224,14 +230,14 @@ __device__ __forceinline__ void half_max(const f32x4 (&sc)[RB][2], float (&mx)[R
 }
 
 // Folds one block, half after half, into O and the sums; false when some row's
-// maximum has outgrown its reference (O is then not whole).  `again` (MASKED only):
+// maximum has outgrown its reference by `limit` (O is then not whole).  `again` (MASKED only):
 // references are the maxima of all blocks, scores are summed from zero, and the
 // result is true.  refill_v and
 // refill_k take quarter `n` of the DMAs into the places of the last block's V and
 // of this one's K; wait_v waits for this block's V.
 template <int RB, int D, bool MASKED, typename WaitV, typename RefillV, typename RefillK>
 __device__ __forceinline__ bool fold_block(Wave8<RB, D>& w, const unsigned char* kp, const unsigned char* vp, float ks,
-                                           float vs, float scale_log2, int key0, int first, int end, bool again,
+                                           float vs, float limit, float scale_log2, int key0, int first, int end, bool again,
                                            WaitV wait_v, RefillV refill_v, RefillK refill_k) {
   const int lg = (threadIdx.x & 63) >> 4;
   const bf16x2 ones = {(__bf16)1.f, (__bf16)1.f};
@@ -258,7 +264,7 @@ __device__ __forceinline__ bool fold_block(Wave8<RB, D>& w, const unsigned char*
     bool grow = false, fresh = false;
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-      grow |= w.m[rb] > kNoKey && mx[rb] * scale_log2 > kGrowLog2;
+      grow |= w.m[rb] > kNoKey && mx[rb] * scale_log2 > limit;
       fresh |= !(w.m[rb] > kNoKey) && mx[rb] > kNoKey;
     }
     if (__builtin_expect(__ballot(grow) != 0, 0) && !known) return false;
@@ -493,8 +499,9 @@ void kv8_attn_kernel(AttnShape s, AttnBatch bt, Kv8Pool pool, int nchunks, const
       static_assert(R::kSlots == 5, "as many as the waits count");
       wait_half(2 * t, Int<3 * R::kOps>());
       done = fold_block<RB, D, MASKED>(
-          w, ring + ks * R::kHalf + off, ring + vs * R::kHalf + off, pow2(ks_all, t), pow2(vs_all, t), s.scale_log2,
-          key_begin + t * kKeyBlock, first, end, again, [&] { wait_half(2 * t + 1, Int<5 * R::kOps / 2>()); },
+          w, ring + ks * R::kHalf + off, ring + vs * R::kHalf + off, pow2(ks_all, t), pow2(vs_all, t),
+          grow_limit(__builtin_amdgcn_readlane(vs_all, t)), s.scale_log2, key_begin + t * kKeyBlock, first, end, again,
+          [&] { wait_half(2 * t + 1, Int<5 * R::kOps / 2>()); },
           [&](int n) {
             if (t > 0 && nv < halves) fetch(nv, last, n * R::kOps / 4, (n + 1) * R::kOps / 4);
           },

@@ -615,3 +615,28 @@ def test_attention_of_scores_far_below_zero(D):
     c.upload()
     got = attend(G, H, H, D, c, lens, q.cuda(), None, 1 / np.sqrt(D))
     assert np.array_equal(got, want)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("exponent", [0, 60, 75, 95])
+def test_attention_of_large_values(exponent, D):
+    """Values up to 2^(exponent + 1) and scores that grow by 40 (2^57.7 in the exponential) after a
+    chunk's first keys: weights times values stay within float32.  One column alone makes a
+    score, as in test_attention_of_scores_that_jump."""
+    G, H, lens = 3, 16, [1400 - 31 * i for i in range(24)]
+    rng = np.random.default_rng(D)
+    c = Cache(rng, lens, H, D, 64)
+    c.ks[...] = 127
+    c.vs[...] = 127 + exponent
+    for b, L in enumerate(lens):
+        k = np.zeros((L, H, D), dtype=np.uint8)
+        k[40::50, :, 0] = 0x62  # 40
+        v = (rng.integers(0x30, 0x40, (L, H, D)) | rng.integers(0, 2, (L, H, D)) << 7).astype(np.uint8)
+        put_rows(c, c.k, fp8.k_index(D), b, k)
+        put_rows(c, c.v, fp8.v_index(D), b, v)
+    c.upload()
+    q = torch.zeros((len(lens), G, H, D), dtype=torch.bfloat16)
+    q[..., 0] = 1.0
+    got = attend(G, H, H, D, c, lens, q.cuda(), None, 1.0)
+    seg = fp8.kv8_segments(c.k, c.v, c.ks, c.vs, c.table, lens)
+    check_attention(got, q.double().numpy(), seg, lens, H, None, 1.0, f"values of 2^{exponent}")
