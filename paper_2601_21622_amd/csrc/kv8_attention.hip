@@ -85,10 +85,16 @@ struct Int {
 
 // LDS DMA of 1 KB: lane l copies 16 bytes from base + off into LDS bytes lds +
 // 16 l (lds wave-uniform).  From inline assembly, so that the compiler adds no
-// waits of its own; the wait state between the write of M0 and the load is here.
+// waits of its own.  The base is copied by a scalar instruction first: that is the
+// wait state between the write of M0 and the load, and the load's base is never a
+// register that a vector instruction (a lane's read, a spill's) wrote just before,
+// which would take five.
 __device__ __forceinline__ void ring_dma(const void* base, uint32_t off, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt"
-               : : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(off), "s"(base) : "m0", "memory");
+  uint64_t from;
+  asm volatile("s_mov_b32 m0, %1\n\ts_mov_b64 %0, %3\n\tglobal_load_lds_dwordx4 %2, %0 nt"
+               : "=&s"(from)
+               : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(off), "s"(base)
+               : "m0", "memory");
 }
 
 __device__ __forceinline__ float max_over_groups(float v) {

@@ -49,19 +49,23 @@ constexpr int stages(int mb, int nw) {
 }
 
 // LDS DMA of 16 (or 4) bytes per lane from base + off into LDS bytes lds + 16 l
-// (4 l), both bases wave-uniform; as line_dma otherwise.
+// (4 l), both bases wave-uniform.  The scalar copy of the base is the wait state
+// between the write of M0 and the load, and the load's base is never a register that a
+// vector instruction wrote just before, which would take five.
 template <bool NT>
 __device__ __forceinline__ void base_dma(const void* base, uint32_t off, uint32_t lds) {
+  uint64_t from;
   if (NT)
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt"
-                 : : "s"(lds), "v"(off), "s"(base) : "m0", "memory");
+    asm volatile("s_mov_b32 m0, %1\n\ts_mov_b64 %0, %3\n\tglobal_load_lds_dwordx4 %2, %0 nt"
+                 : "=&s"(from) : "s"(lds), "v"(off), "s"(base) : "m0", "memory");
   else
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-                 : : "s"(lds), "v"(off), "s"(base) : "m0", "memory");
+    asm volatile("s_mov_b32 m0, %1\n\ts_mov_b64 %0, %3\n\tglobal_load_lds_dwordx4 %2, %0"
+                 : "=&s"(from) : "s"(lds), "v"(off), "s"(base) : "m0", "memory");
 }
 __device__ __forceinline__ void base_dma_word(const void* base, uint32_t off, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
-               : : "s"(lds), "v"(off), "s"(base) : "m0", "memory");
+  uint64_t from;
+  asm volatile("s_mov_b32 m0, %1\n\ts_mov_b64 %0, %3\n\tglobal_load_lds_dword %2, %0"
+               : "=&s"(from) : "s"(lds), "v"(off), "s"(base) : "m0", "memory");
 }
 
 template <int X>
