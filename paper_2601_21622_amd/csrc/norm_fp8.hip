@@ -9,6 +9,8 @@
 // 92 us, 5.6 TB/s (a large copy reaches 4.9), 48 rows of 4,096 3.4 us, a launch's
 // latency and two trips to memory.  Squares are summed in float64: float32 squares
 // of values past 1.8e19 overflow, and the conversions hide behind the loads.
+#include <algorithm>
+
 #include "fp8.h"
 
 namespace sdv {
@@ -60,7 +62,7 @@ __device__ __forceinline__ float row_max(float v) {
 
 template <typename T, int THREADS, int R>
 __global__ __launch_bounds__(THREADS)
-void residual_norm_kernel(int rows, int width, float eps, const T* x, const T* residual, const T* __restrict__ weight,
+void residual_norm_kernel(int scale_stride, int width, float eps, const T* x, const T* residual, const T* __restrict__ weight,
                           T* new_residual, uint8_t* __restrict__ out, float* __restrict__ out_scale) {
   constexpr int NW = THREADS / kWave;
   __shared__ double part[NW];
@@ -117,7 +119,7 @@ void residual_norm_kernel(int rows, int width, float eps, const T* x, const T* r
       const u32x2 c = {encode4(y[0] * to, y[1] * to, y[2] * to, y[3] * to),
                        encode4(y[4] * to, y[5] * to, y[6] * to, y[7] * to)};
       *reinterpret_cast<u32x2*>(out + base + g * 8) = c;
-      if ((t & 15) == 0) out_scale[(int64_t)(g / 16) * rows + row] = s;
+      if ((t & 15) == 0) out_scale[(int64_t)(g / 16) * scale_stride + row] = s;
     }
   }
 }
@@ -131,17 +133,23 @@ hipError_t launch_residual_norm(bool f32, int rows, int width, float eps, const 
   // Few groups per thread, few idle threads.  30,000 rows of 4,096: 149 us with 256
   // threads of two groups, 154 with 512 of one, 155 with 128 of four; of 8,192: 296 with 512
   // of two, 302 with 256 of four, 312 with 1,024 of one.
+  // A launch's threads number less than 2^32, so that many rows are several launches.
 #define SDV_NORM(T, N, R)                                                                                             \
-  hipLaunchKernelGGL((residual_norm_kernel<T, N, R>), dim3(rows), dim3(N), 0, stream, rows, width, eps,               \
-                     static_cast<const T*>(x), static_cast<const T*>(residual), static_cast<const T*>(weight),        \
-                     static_cast<T*>(new_residual), out, out_scale)
+  for (int r0 = 0; r0 < rows; r0 += (1 << 30) / N) {                                                                  \
+    const int64_t at = (int64_t)r0 * width;                                                                           \
+    const T* const res = residual != nullptr ? static_cast<const T*>(residual) + at : nullptr;                        \
+    T* const next = new_residual != nullptr ? static_cast<T*>(new_residual) + at : nullptr;                           \
+    hipLaunchKernelGGL((residual_norm_kernel<T, N, R>), dim3(std::min(rows - r0, (1 << 30) / N)), dim3(N), 0, stream, \
+                       rows, width, eps, static_cast<const T*>(x) + at, res, static_cast<const T*>(weight), next,     \
+                       out + at, out_scale + r0);                                                                     \
+  }
 #define SDV_NORM_SIZES(T)                            \
-  if (groups <= 64) SDV_NORM(T, 64, 1);              \
-  else if (groups <= 256) SDV_NORM(T, 256, 1);       \
-  else if (groups <= 512) SDV_NORM(T, 256, 2);       \
-  else if (groups <= 1024) SDV_NORM(T, 512, 2);      \
-  else if (groups <= 2048) SDV_NORM(T, 1024, 2);     \
-  else SDV_NORM(T, 1024, 4);
+  if (groups <= 64) SDV_NORM(T, 64, 1)               \
+  else if (groups <= 256) SDV_NORM(T, 256, 1)        \
+  else if (groups <= 512) SDV_NORM(T, 256, 2)        \
+  else if (groups <= 1024) SDV_NORM(T, 512, 2)       \
+  else if (groups <= 2048) SDV_NORM(T, 1024, 2)      \
+  else SDV_NORM(T, 1024, 4)
   if (f32) {
     SDV_NORM_SIZES(float)
   } else {

@@ -228,3 +228,23 @@ def test_the_calls_as_one_step():
         for b in range(B):
             pool.truncate(b, int(start[b]))
     pool.close()
+
+
+def test_norm_of_more_rows_than_a_launch_holds():
+    """2^24 rows of 256 threads each: a launch holds fewer than 2^32 threads.  Every stretch of equal rows
+    comes out as the first, which is the small call's."""
+    width, part, times = 544, 1 << 14, 1 << 10
+    rng = np.random.default_rng(5)
+    few = torch.from_numpy(rng.normal(size=(part, width))).bfloat16().cuda()
+    w = torch.from_numpy(rng.normal(size=(width,))).bfloat16().cuda()
+    x = torch.empty((times, part, width), dtype=torch.bfloat16, device="cuda")
+    x.copy_(few[None])
+    out = torch.zeros((times * part, width), dtype=torch.uint8, device="cuda")
+    scale = torch.zeros((-(-width // 128), times * part), device="cuda")
+    flat = x.view(times * part, width)
+    sd.sd_residual_norm_fp8(flat, None, w, 1e-5, flat, out.view(F8), scale)
+    one, one_scale = torch.empty((part, width), dtype=torch.uint8, device="cuda"), torch.empty((scale.shape[0], part), device="cuda")
+    sd.sd_residual_norm_fp8(few, None, w, 1e-5, None, one.view(F8), one_scale)
+    for i in range(times):
+        at = slice(i * part, (i + 1) * part)
+        assert torch.equal(out[at], one) and torch.equal(scale[:, at], one_scale) and torch.equal(x[i], few), i
