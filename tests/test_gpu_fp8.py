@@ -248,3 +248,21 @@ def test_norm_of_more_rows_than_a_launch_holds():
     for i in range(times):
         at = slice(i * part, (i + 1) * part)
         assert torch.equal(out[at], one) and torch.equal(scale[:, at], one_scale) and torch.equal(x[i], few), i
+
+
+def test_norm_divides_by_the_scale():
+    """Codes are those of y / s, ties to even: rows of ones (their mean square is one, y is the
+    weight) and weights that lie halfway between two codes' values of their block's scale, to the bit."""
+    width = 32768
+    rng = np.random.default_rng(6)
+    s = np.repeat(rng.integers(1 << 14, 1 << 15, width // 128) / 2.0 ** 15, 128)  # 15 bits: 448 s and tie s are exact
+    halves = (fp8.VALUES[8:126] + fp8.VALUES[9:127]) / 2
+    z = rng.choice(halves, width) * rng.choice([-1.0, 1.0], width)
+    z[::128] = 448.0
+    w = (z * s).astype(np.float32)
+    assert np.array_equal(w.astype(np.float64), z * s)
+    x = torch.ones((2, width), device="cuda")
+    x[1, ::3] = -1
+    _, code, scale = run_norm(x, None, torch.from_numpy(w).cuda(), 0.0)
+    assert np.array_equal(scale, np.repeat(s[::128, None], 2, axis=1))
+    assert np.array_equal(code, fp8.encode(z[None] * x.cpu().double().numpy()))
