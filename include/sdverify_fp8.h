@@ -128,7 +128,7 @@ SD_API int sd_verify_attention_kv8(const sd_dims_t* dims, const void* q, const s
  *   out_scale  [ceil(width/128)][rows] float32: sd_verify_logits_fp8's hidden_scale
  * width: a multiple of 32, at most 32768 (SD_ERR_UNSUPPORTED otherwise); rows 1 .. 2^24.
  * A NaN or an infinity in h makes the row's codes NaN or, where h is finite
- * beside an infinity, 0; the scale stays a number.
+ * beside an infinity, 0; the scale stays a number.  So do zeros with eps 0 (0 / 0).
  */
 typedef struct {
   int32_t rows;

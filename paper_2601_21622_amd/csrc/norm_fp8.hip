@@ -108,12 +108,19 @@ void residual_norm_kernel(int scale_stride, int width, float eps, const T* x, co
 #pragma unroll
     for (int w = 1; w < NW; ++w) sum += part[w];
   }
-  const float inv = (float)(1.0 / sqrt(sum / (double)width + (double)eps));
+  // 1/rms as inv * up: rows near float32's ends have one that is no normal float32.
+  const double by = 1.0 / sqrt(sum / (double)width + (double)eps);
+  const float up = by > 0x1p100 ? 0x1p64f : by < 0x1p-100 ? 0x1p-64f : 1.f;
+  const float inv = (float)(by / (double)up);
 #pragma unroll
   for (int i = 0; i < R; ++i) {
     const int g = t + i * THREADS;
     const bool live = g < groups;
     if (live && new_residual != nullptr) store8(new_residual + base + g * 8, h[i]);
+    if (up != 1.f) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) h[i][e] *= up;
+    }
     float w[8], y[8], most = 0.f;
     load8(weight + min(g, groups - 1) * 8, w);
 #pragma unroll

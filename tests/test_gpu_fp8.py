@@ -266,3 +266,19 @@ def test_norm_divides_by_the_scale():
     _, code, scale = run_norm(x, None, torch.from_numpy(w).cuda(), 0.0)
     assert np.array_equal(scale, np.repeat(s[::128, None], 2, axis=1))
     assert np.array_equal(code, fp8.encode(z[None] * x.cpu().double().numpy()))
+
+
+@pytest.mark.parametrize("exponent,dtype", [(-140, torch.float32), (-126, torch.float32), (-110, torch.float32), (110, torch.float32),
+                                            (125, torch.float32), (-120, torch.bfloat16), (125, torch.bfloat16)])
+def test_norm_of_rows_near_the_ends_of_float32(exponent, dtype):
+    """Rows of magnitude 2^exponent and eps 0: the normed rows are of magnitude one.  The bounds of test_norm."""
+    rng = np.random.default_rng(200 + exponent)
+    x = torch.from_numpy(np.clip(rng.normal(size=(5, 544)), -3, 3) * 2.0 ** exponent).to(dtype)
+    w = torch.from_numpy(rng.normal(size=(544,))).to(dtype)
+    new, code, scale = run_norm(x.cuda(), None, w.cuda(), 0.0)
+    assert torch.equal(new.cpu(), x)
+    _, y, s = fp8.residual_norm(x.double().numpy(), None, w.double().numpy(), 0.0)
+    assert np.all(np.abs(scale - s) <= 8 * U * s)
+    z = y / np.repeat(scale.T, 128, axis=1)[:, :544]
+    step = 2.0 ** (np.maximum(np.floor(np.log2(np.maximum(np.abs(z), 1e-30))), -6) - 3)
+    assert np.all(np.abs(fp8.decode(code) - z) <= step / 2 + 16 * U * np.abs(z))
