@@ -53,7 +53,7 @@ extern "C" {
  *            e4m3: key 16 t + 4 g + r of the block, column 16 i + d
  *   k_scale, v_scale  [num_pages][n_kv_heads][page_size/64] exponent bytes: a
  *            code stands for code * 2^(byte - 127).  sd_kv8_append writes bytes
- *            27 .. 247; the attention takes 1 .. 254.
+ *            27 .. 247 (or a block's larger one); both calls take 1 .. 254.
  * k and v 16-byte aligned, block_table 4-byte aligned.
  */
 typedef struct {

@@ -39,8 +39,8 @@ __device__ __forceinline__ int scale_byte(float most) {
   return max(e, kLowestExp);
 }
 
-__device__ __forceinline__ float pow2_f32(int e) {  // 2^e, -126 <= e <= 127
-  return __uint_as_float((uint32_t)(e + 127) << 23);
+__device__ __forceinline__ float pow2_f32(int e) {  // 2^e, -127 <= e <= 127
+  return __uint_as_float(e > -127 ? (uint32_t)(e + 127) << 23 : 0x400000u);
 }
 
 template <typename T>

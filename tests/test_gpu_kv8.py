@@ -640,3 +640,24 @@ def test_attention_of_large_values(exponent, D):
     got = attend(G, H, H, D, c, lens, q.cuda(), None, 1.0)
     seg = fp8.kv8_segments(c.k, c.v, c.ks, c.vs, c.table, lens)
     check_attention(got, q.double().numpy(), seg, lens, H, None, 1.0, f"values of 2^{exponent}")
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("new", [3, 20])
+def test_append_to_blocks_of_any_scale(new, dim):
+    """Blocks that other programs filled hold any scale byte from 1 to 254."""
+    rng = np.random.default_rng(new)
+    bytes_ = [1, 2, 20, 26, 27, 100, 240, 247, 248, 252, 253, 254]
+    lens = [40 + new] * len(bytes_)
+    c = Cache(rng, lens, 2, dim, 64)
+    for b, v in enumerate(bytes_):
+        c.ks[c.table[b, 0]] = v
+        c.vs[c.table[b, 0]] = v
+    c.upload()
+    x = [(rng.uniform(1, 2, (new, 2, dim)) * 2.0 ** rng.choice([-120, -3, 60, 127], (new, 2, dim))).astype(np.float32) for _ in range(2)]
+    d = sd.Dims(len(lens), 0, 2, 2, dim, 32, 1, 0, 0)
+    off, n = [0] * len(lens), [new] * len(lens)
+    c.append(*(a.astype(np.float64) for a in x), off, n, lens)
+    sd.sd_kv8_append(d, c.handle, *(torch.from_numpy(a).cuda() for a in x), off, n, lens)
+    torch.cuda.synchronize()
+    c.check()
