@@ -59,7 +59,10 @@ class KV8Cache(ctypes.Structure):
         c._tensors = (k, v, k_scale, v_scale, block_table)
         c._heads = int(k_scale.shape[1])
         c._rows = int(block_table.shape[0])
-        c._dim = k.numel() // max(1, int(k.shape[0]) * c._heads * page_size)
+        rows = int(k.shape[0]) * c._heads * page_size
+        c._dim = k.numel() // max(1, rows)
+        if c._dim * rows != k.numel():
+            raise ValueError("a pool's size is not pages * heads * page_size * head_dim")
         c._device = _device(c._tensors)
         c._ref = ctypes.byref(c)
         return c

@@ -661,3 +661,15 @@ def test_append_to_blocks_of_any_scale(new, dim):
     sd.sd_kv8_append(d, c.handle, *(torch.from_numpy(a).cuda() for a in x), off, n, lens)
     torch.cuda.synchronize()
     c.check()
+
+
+def test_a_pool_of_another_size_is_refused():
+    """Pages with bytes to spare would be read at the wrong places."""
+    rng = np.random.default_rng(16)
+    c = filled(rng, [64], 2, 64, 64)
+    n = c.dev[0].shape[0]
+    k, v = (torch.zeros((n, 2 * 64 * 64 + extra), dtype=torch.uint8, device="cuda") for extra in (64, 64))
+    with pytest.raises(ValueError):
+        sd.KV8Cache.of(k, v, c.dev[2], c.dev[3], c.handle._tensors[4], 64)
+    k, v = (t[:, :2 * 64 * 64].contiguous() for t in (k, v))
+    sd.KV8Cache.of(k, v, c.dev[2], c.dev[3], c.handle._tensors[4], 64)
