@@ -282,3 +282,16 @@ def test_norm_of_rows_near_the_ends_of_float32(exponent, dtype):
     z = y / np.repeat(scale.T, 128, axis=1)[:, :544]
     step = 2.0 ** (np.maximum(np.floor(np.log2(np.maximum(np.abs(z), 1e-30))), -6) - 3)
     assert np.all(np.abs(fp8.decode(code) - z) <= step / 2 + 16 * U * np.abs(z))
+
+
+@pytest.mark.parametrize("V", [900, 33001])
+def test_logits_of_a_row_among_other_rows(V):
+    """A row's logits and log-sum-exp are the same bits at another place of a tile of the same shape, beside fewer rows."""
+    rng = np.random.default_rng(V)
+    a, w = random_codes(rng, (64, 544)), random_codes(rng, (V, 544))
+    sa, sw = rng.random((5, 64)).astype(np.float32), rng.random((-(-V // 128), 5)).astype(np.float32)
+    every, lse = run_logits(a, sa, w, sw)
+    for n in (64, 40, 33):
+        pick = rng.permutation(64)[:n]
+        got, got_lse = run_logits(a[pick], sa[:, pick], w, sw)
+        assert np.array_equal(got, every[pick]) and np.array_equal(got_lse, lse[pick]), n
