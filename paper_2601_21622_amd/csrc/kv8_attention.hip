@@ -635,14 +635,20 @@ int64_t cu_count() {
 // 16-row blocks of a wave.  One holds up to five (at head dimension 128 O takes 32
 // registers of each, Q 16); more rows are split over row groups, a wave each.  Where the
 // caches are a few blocks of keys per place, what counts is how long a wave takes for
-// its own: two row blocks, or one where three would leave a wave half empty, and
-// the groups read the same keys from L2.  `blocks`: 64-key blocks times heads.
-// 64 rows, D = 128, 8 heads: 4 requests of 1,500 keys (768 blocks) 17.9 us so and 22.0
-// with four row blocks, 16 of 3,000 (6,016) 43.9 and 45.6, 64 of 2,000 (16,384) 87.7 and
-// 77.1; 48 rows, D = 64, 13 of 1,500 (2,496) 18.7 with one, 20.9 with two, 19.9 with three.
-int row_groups(int rows, int64_t blocks) {
+// its own: two row blocks, or one where there are three (two would leave a wave half
+// empty, which costs more than a third wave; of five and more they do not), and
+// the groups read the same keys from L2.  `blocks`: 64-key blocks times heads, few up to
+// 10 per CU at D = 128 and 32 at 64, where twice as many waves run at once.
+// 8 heads, 4 and 24 requests of one length, us with one or two row blocks / with all:
+//   D = 128, 48 rows:  2,000 blocks 25, 29 / 25, 28; 3,200 31, 40 / 33, 32; 6,000 47, 66 / 40, 41
+//            72 rows:  2,000 30, 35 / 34, 33; 3,200 37, 47 / 39, 40; 6,000 56, 77 / 49, 51
+//   D = 64,  48 rows:  2,000 18, 17 / 20, 18; 6,000 29, 30 / 33, 31; 8,100 35, 36 / 37, 34
+//            72 rows:  2,000 21, 22 / 28, 26; 6,000 36, 36 / 45, 42; 8,100 44, 45 / 49, 46
+// 4 requests of 1,500 keys, D = 128, one and two row blocks: 40 rows 15.2 and 16.2, 72 rows
+// 21.2 and 19.6, 112 rows 27.7 and 23.0.
+int row_groups(int rows, int D, int64_t blocks) {
   const int b = (rows + 15) / 16;
-  const int most = blocks > 32 * cu_count() ? kMaxBlocks : b == 3 ? 1 : 2;
+  const int most = blocks > (D == 64 ? 32 : 10) * cu_count() ? kMaxBlocks : b == 3 ? 1 : 2;
   return (b + most - 1) / most;
 }
 int blocks_of(int rows, int groups) { return ((rows + 15) / 16 + groups - 1) / groups; }
@@ -662,7 +668,7 @@ AttnShape kv8_shape(int G, int Hq, int Hkv, int D, float scale, const int32_t* k
   s.rows = G * s.group;
   int64_t blocks = 0;
   for (int b = 0; b < B; ++b) blocks += (kv_len[b] + kKeyBlock - 1) / kKeyBlock;
-  s.row_groups = row_groups(s.rows, blocks * Hkv);
+  s.row_groups = row_groups(s.rows, D, blocks * Hkv);
   s.scale_log2 = scale * kLog2e;
   // For a half to four rounds of items over the CUs' places the shortest chunk that
   // fits them; of these the one that is done first, counted in keys of a wave with up to
