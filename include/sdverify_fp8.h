@@ -120,7 +120,9 @@ SD_API int sd_verify_attention_kv8(const sd_dims_t* dims, const void* q, const s
  * Residual, norm and 8-bit output of `rows` rows of `width` columns:
  *   h = x + residual, new_residual = h in dtype, y = h * weight / sqrt(mean(h^2) + eps),
  *   and per row and 128 columns: s = max(max|y| / 448, 2^-126), code = y / s in e4m3.
- * y is formed from the unrounded h, in float32; the mean in float64.
+ * y is formed from the unrounded h; the mean in float64, the rest in float32.  1/rms
+ * divides out of y / s: a code is the nearest to h * weight / (max|h * weight| / 448),
+ * three float32 roundings.
  *   x, residual, new_residual  [rows][width] in dtype; residual NULL: h = x;
  *            new_residual NULL: not stored.  new_residual may be x or residual.
  *   weight   [width] in dtype

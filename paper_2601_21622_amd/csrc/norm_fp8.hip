@@ -62,8 +62,8 @@ __device__ __forceinline__ float row_max(float v) {
 
 // y / s, rounded to nearest, with the rounded reciprocal of s: the remainder of the
 // first product is exact and corrects it (Markstein's division step).  Its sign is
-// taken so that a zero keeps y's.  2,000 rows of 4,096: 12.3 us so, 11.9 with the product
-// alone, 14.3 with the division's instructions.
+// taken so that a zero keeps y's.  2,000 rows of 4,096: 12.7 us so, 12.3 with the product
+// alone, 14.7 with the division's instructions.
 __device__ __forceinline__ float quotient(float y, float s, float to) {
   const float q = y * to;
   return fmaf(-fmaf(q, s, -y), to, q);
@@ -74,7 +74,7 @@ __global__ __launch_bounds__(THREADS)
 void residual_norm_kernel(int scale_stride, int width, float eps, const T* x, const T* residual, const T* __restrict__ weight,
                           T* new_residual, uint8_t* __restrict__ out, float* __restrict__ out_scale) {
   constexpr int NW = THREADS / kWave;
-  __shared__ double part[NW];
+  __shared__ double sums[NW];
   const int row = blockIdx.x, t = threadIdx.x;
   const int groups = width / 8;
   const int64_t base = (int64_t)row * width;
@@ -102,41 +102,48 @@ void residual_norm_kernel(int scale_stride, int width, float eps, const T* x, co
     }
   sum = wave_sum_f64(sum);
   if (NW > 1) {
-    if ((t & 63) == 0) part[t >> 6] = sum;
+    if ((t & 63) == 0) sums[t >> 6] = sum;
     __syncthreads();
-    sum = part[0];
+    sum = sums[0];
 #pragma unroll
-    for (int w = 1; w < NW; ++w) sum += part[w];
+    for (int w = 1; w < NW; ++w) sum += sums[w];
   }
-  // 1/rms as inv * up: rows near float32's ends have one that is no normal float32.
+  // 1/rms as inv * up, up a power of two: h * up is exact, and codes are those of
+  // v / (max|v| / 448), v = h * up * weight: three roundings, and inv enters the scale
+  // alone.  Rows of subnormal numbers are lifted first.  Infinities, NaN, and zeros with
+  // eps 0: h * up is 0 or NaN as h / rms is.
   const double by = 1.0 / sqrt(sum / (double)width + (double)eps);
-  const float up = by > 0x1p100 ? 0x1p64f : by < 0x1p-100 ? 0x1p-64f : 1.f;
-  const float inv = (float)(by / (double)up);
+  const bool number = by > 0.0 && by < (double)INFINITY;
+  const int e = number ? max(ilogb(by), -126) : 0;
+  const bool lift = e > 126;
+  const float up = number ? ldexpf(1.f, lift ? e - 64 : e) : (float)by;
+  const float inv = number ? (float)ldexp(by, -e) : 1.f;
+  const float least = 0x1p-126f / inv;
 #pragma unroll
   for (int i = 0; i < R; ++i) {
     const int g = t + i * THREADS;
     const bool live = g < groups;
     if (live && new_residual != nullptr) store8(new_residual + base + g * 8, h[i]);
-    if (up != 1.f) {
+    if (lift) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) h[i][e] *= up;
+      for (int e = 0; e < 8; ++e) h[i][e] *= 0x1p64f;
     }
-    float w[8], y[8], most = 0.f;
+    float w[8], v[8], most = 0.f;
     load8(weight + min(g, groups - 1) * 8, w);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      y[e] = h[i][e] * inv * w[e];
-      most = fmaxf(most, live ? fabsf(y[e]) : 0.f);
+      v[e] = h[i][e] * up * w[e];
+      most = fmaxf(most, live ? fabsf(v[e]) : 0.f);
     }
     most = row_max(most);
-    const float s = fmaxf(most / 448.f, 0x1p-126f);
+    const float part = most / 448.f, s = fmaxf(part, least);
     const float to = 1.f / s;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = quotient(y[e], s, to);
+    for (int e = 0; e < 8; ++e) v[e] = quotient(v[e], s, to);
     if (live) {
-      const u32x2 c = {encode4(y[0], y[1], y[2], y[3]), encode4(y[4], y[5], y[6], y[7])};
+      const u32x2 c = {encode4(v[0], v[1], v[2], v[3]), encode4(v[4], v[5], v[6], v[7])};
       *reinterpret_cast<u32x2*>(out + base + g * 8) = c;
-      if ((t & 15) == 0) out_scale[(int64_t)(g / 16) * scale_stride + row] = s;
+      if ((t & 15) == 0) out_scale[(int64_t)(g / 16) * scale_stride + row] = fmaxf(part * inv, 0x1p-126f);
     }
   }
 }

@@ -295,3 +295,46 @@ def test_logits_of_a_row_among_other_rows(V):
         pick = rng.permutation(64)[:n]
         got, got_lse = run_logits(a[pick], sa[:, pick], w, sw)
         assert np.array_equal(got, every[pick]) and np.array_equal(got_lse, lse[pick]), n
+
+
+def test_norm_codes_of_short_numbers():
+    """bf16 rows and weights: h * weight is exact in float32, so codes are those of its quotient by the
+    block's largest over 448, whatever 1 / rms is; a block of zeros has scale 2^-126 and codes 0."""
+    rng = np.random.default_rng(7)
+    x = torch.from_numpy(rng.normal(size=(300, 1024)) * 2.0 ** rng.choice([-140, -100, -3, 0, 60, 120], (300, 1))).bfloat16()
+    w = torch.from_numpy(rng.normal(size=(1024,))).bfloat16()
+    w[128:256] = 0
+    for eps in (0.0, 1e-5):
+        _, code, scale = run_norm(x.cuda(), None, w.cuda(), eps)
+        v = x.double().numpy() * w.double().numpy()
+        most = np.abs(v).reshape(300, 8, 128).max(axis=2)
+        z = v / np.maximum(np.repeat(most, 128, axis=1) / 448, 1e-300)
+        # Two roundings of the quotient, 2^-24 each: only values so near a halfway point may go either way.
+        low, high = fp8.encode(z * (1 - 2.5 * U)), fp8.encode(z * (1 + 2.5 * U))
+        none = (x.double().numpy() == 0).all(axis=1)  # bfloat16 ends at 2^-133: rows of zeros, 0 / 0 with eps 0
+        assert 0 < none.sum() < 100
+        if eps == 0.0:
+            assert (code[none] & 127 == 127).all() and (scale[:, none] == 2.0 ** -126).all()
+        ok = (code == low) | (code == high) | ((z == 0) & (code & 127 == 0))
+        assert ok[~none | (eps > 0)].all()
+        assert (scale[1] == 2.0 ** -126).all()
+        assert (low != high).mean() < 1e-3
+
+
+def test_norm_codes_do_not_depend_on_the_mean():
+    """As test_norm_divides_by_the_scale, with rows of ones and twos: 1 / rms is no short number, but
+    it divides out of y / s, and the codes are those of the exact halfway values, to the bit."""
+    width = 32768
+    rng = np.random.default_rng(8)
+    s = np.repeat(rng.integers(1 << 14, 1 << 15, width // 128) / 2.0 ** 15, 128)
+    halves = (fp8.VALUES[8:126] + fp8.VALUES[9:127]) / 2
+    z = rng.choice(halves, width) * rng.choice([-1.0, 1.0], width)
+    z[::128] = 448.0
+    h = rng.choice([1.0, 2.0], width)
+    w = (z * s / h).astype(np.float32)
+    assert np.array_equal(w.astype(np.float64) * h, z * s)
+    x = torch.from_numpy(np.stack([h, -h, h * 2.0 ** 30, h * 2.0 ** -130])).float().cuda()
+    _, code, scale = run_norm(x, None, torch.from_numpy(w).cuda(), 0.0)
+    assert np.array_equal(code, fp8.encode(z[None] * np.sign(x.cpu().double().numpy())))
+    want = (s[::128] / np.sqrt((h * h).mean()))[:, None]
+    assert np.all(np.abs(scale - want) <= 4 * U * want)
