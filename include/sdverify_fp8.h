@@ -14,7 +14,9 @@
  *                            weights, and the rows' log-sum-exp, as
  *                            sd_accept_resample and its kin take them
  * Products and sums are float32: codes widen to bfloat16 exactly, their
- * products are exact, and scales enter in float32.
+ * products are exact, and scales enter in float32.  The attention's weights
+ * exp(score - maximum) are rounded to bfloat16 where they multiply V, and the
+ * sum that divides adds the rounded ones.
  *
  * The conventions of sdverify.h hold: device pointers unless marked (host),
  * argument checks on the host before anything is enqueued, no allocation, no
@@ -24,7 +26,8 @@
  * Work is enqueued on `stream`, which belongs to the current device, as do all
  * buffers.
  * sd_dims_t is used with these differences: gamma may be 0 (one position per
- * request: plain decoding), flags must be 0, and a call reads only the fields
+ * request: plain decoding, whose token the caller draws from the logits, since
+ * acceptance takes gamma >= 1), flags must be 0, and a call reads only the fields
  * that it lists.
  */
 #ifndef SDVERIFY_FP8_H
@@ -90,6 +93,10 @@ SD_API size_t sd_fp8_workspace_bytes(const sd_dims_t* dims, int32_t max_kv_len);
  * rounded to nearest, ties to even; infinities and NaN become NaN.  Bytes of keys
  * from kv_len on keep their values; other pages are not touched.  The pages that
  * a call writes belong to one request each; calls on one cache run one after another.
+ * A block's scale never shrinks while it holds earlier keys.  A rejected draft that raised it
+ * has requantised the earlier keys of its block, and they stay so after the cut back:
+ * values below 2^-6 of the new scale keep fewer fraction bits than in a cache that
+ * never saw the draft.  Acceptance is lossless with respect to the logits of the cache as it is.
  */
 SD_API int sd_kv8_append(const sd_dims_t* dims, const sd_kv8_cache_t* cache, const void* k_new, int64_t k_stride,
                          const void* v_new, int64_t v_stride, const int64_t* new_off, const int32_t* new_len,
@@ -105,7 +112,8 @@ SD_API int sd_kv8_append(const sd_dims_t* dims, const sd_kv8_cache_t* cache, con
  *            keys are this step's positions, appended before
  *   parent   NULL, or [B][gamma] int32 (device) as in sd_verify_attention_tree.
  *            After acceptance, append the accepted nodes' rows again, from
- *            key kv_len - gamma on: that is the cache's commit.
+ *            key kv_len - gamma on: that is the cache's commit.  Their rows, which the
+ *            caller kept, have to be gathered first: an append takes consecutive rows.
  *   scale    softmax scale, finite and > 0
  * G * (n_q_heads / n_kv_heads) <= 128.  Keys that a position does not see
  * contribute nothing, whatever they hold; a NaN that it sees makes its output NaN.
