@@ -9,9 +9,10 @@
 //
 // Bound by the cache's stream up to two 16-row blocks: 16 requests of 24,576 keys, 8 KV
 // heads, D = 128 (805 MB) take 128-133 us with one block, 6.1-6.3 TB/s, and 145 with
-// two.  Each block more adds about 21 us (187 with four, 206 with five), of which the vector
-// instructions of its 64 x 16 scores are the larger part and its matrix products
-// 12: LDS and registers allow one wave per SIMD there, and its phases follow one another.
+// two.  Each block more adds about 20 us (152 with three, 178 with four, 200 with five), of
+// which the vector instructions of its 64 x 16 scores are the larger part and its matrix
+// products 12: LDS and registers allow one wave per SIMD there, and its phases follow one
+// another.
 // Scores are kept in vector registers by the build's choice of instruction form: in
 // accumulation registers every score is moved once more (four blocks 194 us, five 214).
 //
@@ -367,8 +368,8 @@ __device__ __forceinline__ void spread_nan(Wave8<RB, D>& w, const unsigned char*
 }
 
 // At head dimension 64 LDS holds two waves per SIMD, and half the registers each are
-// enough (five blocks spill 36): 16 requests of 24,576 keys, 8 heads: of 64 rows 105 us,
-// 133 with one wave per SIMD; of 72 rows 118 and 149.
+// enough (five blocks spill 52): 16 requests of 24,576 keys, 8 heads: of 64 rows 105 us,
+// 133 with one wave per SIMD; of 72 rows 118-126 and 149.
 template <int RB, int D>
 __global__ __launch_bounds__(kWave, D == 64 ? 2 : 1)
 void kv8_attn_kernel(AttnShape s, AttnBatch bt, Kv8Pool pool, int nchunks, const uint16_t* __restrict__ q,

@@ -6,9 +6,9 @@
 // exponentials, folded into the rows' log-sum-exp by the bf16 projection's kernel.
 //
 // Bound by the stream of W up to about 64 rows (1.05 GB for 64 x 128,256 x 8,192 in 192
-// us, 5.5 TB/s), by the matrix cores' power past that: 224 x 128,256 x 4,096 takes 236 us,
-// 1.0 PFLOP/s, where a large bfloat16 product of the library reaches 1.2 on the same card,
-// and the same launch over codes that are all zero, with nothing else changed, takes 191.
+// us, 5.5 TB/s), by the matrix cores' power past that: 224 x 128,256 x 4,096 takes 245 us,
+// 0.96 PFLOP/s, where a large bfloat16 product of the library reaches 1.14 to 1.2 on the same
+// card, and the same launch over codes that are all zero, with nothing else changed, takes 184.
 // A row's 128 columns of one scale are one 128-byte line, so W [V][K] and the
 // rows [M][K] are streamed as they are, in whole lines by LDS DMA, a line of
 // every row of the tile per stage.  Codes widen to bfloat16 exactly on their way
@@ -186,8 +186,8 @@ void vocab_fp8_kernel(int M, int K, int V, int ntiles, int mtiles, const uint8_t
   int s = 0, left = nlines;
   // One line: the products of its 128 columns, from zero, times both scales.
   // FILL: it asks for rows and entries (2), for rows (1) or for nothing (0), bit by bit
-  // between the products: a CU keeps about 100 lines in flight, and a wave that asks
-  // for more stands still.
+  // between the products: a wave that asks for a whole stage at once stands still
+  // while the CU's lines in flight (65 on average with 6 rows of 4,096) make room.
   auto line = [&](auto fill) {
     constexpr int kFill = decltype(fill)::value;
     // The line is in once only what was asked for after its rows is in flight.
