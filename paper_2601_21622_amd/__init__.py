@@ -1,8 +1,8 @@
 """Batched, lossless speculative verification on one MI355X (gfx950).
 
 Thin ctypes binding of ``libsdverify.so`` (the C-ABI declared in
-``include/sdverify.h``, and for 8-bit caches and weights in
-``include/sdverify_fp8.h``).  Each function has the C name, marshals torch device
+``include/sdverify.h``, for 8-bit caches and weights in ``include/sdverify_fp8.h`` and
+for 4-bit caches in ``include/sdverify_fp4.h``).  Each function has the C name, marshals torch device
 tensors, host integer arrays and the current HIP stream into the C call, and
 raises :class:`SdError` on a non-zero status.  No step of the computation runs
 in Python: every result comes from the HIP kernels, and the binding fails
@@ -68,4 +68,16 @@ from ._fp8 import (  # noqa: F401
     sd_residual_norm_fp8,
     sd_verify_attention_kv8,
     sd_verify_logits_fp8,
+)
+from ._fp4 import (  # noqa: F401
+    SD_KV4_BLOCK,
+    SD_KV4_GROUP,
+    KV4Cache,
+    Rope,
+    exported_fp4_symbols,
+    sd_kv4_append,
+    sd_kv4_read,
+    sd_kv4_workspace_bytes,
+    sd_qk_norm_rope,
+    sd_verify_attention_kv4,
 )

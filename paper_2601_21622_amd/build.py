@@ -17,8 +17,9 @@ CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libsdverify.so")
 SOURCES = ["api.hip", "attention.hip", "vocab.hip", "lines.hip", "rows.hip", "accept.hip", "warp.hip", "rate.hip", "pool.hip", "expand.hip",
-           "kv8_append.hip", "kv8_attention.hip", "norm_fp8.hip", "vocab_fp8.hip"]
-HOST_SOURCES = ["fp8_api.hip"]  # no kernels of their own
+           "kv8_append.hip", "kv8_attention.hip", "norm_fp8.hip", "vocab_fp8.hip", "kv4_rows.hip", "kv4_attention.hip",
+           "qk_rope.hip"]
+HOST_SOURCES = ["fp8_api.hip", "fp4_api.hip"]  # no kernels of their own
 ARCH = "gfx950"
 
 HIPCC_FLAGS = [
@@ -44,6 +45,7 @@ EXTRA_FLAGS = {
     # option of the compiler's own, which changes where results are held and nothing of them;
     # without it the kernels are right and up to 4 % slower.
     "kv8_attention.hip": ["-fno-honor-nans", "-mno-amdgpu-ieee", "-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+    "kv4_attention.hip": ["-fno-honor-nans", "-mno-amdgpu-ieee", "-mllvm", "-amdgpu-mfma-vgpr-form=1"],
 }
 
 

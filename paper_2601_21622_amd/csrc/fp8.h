@@ -43,6 +43,10 @@ AttnShape kv8_shape(int G, int Hq, int Hkv, int D, float scale, const int32_t* k
 int64_t kv8_max_chunks(int Hkv, int D, int B, int64_t max_kv_len);
 hipError_t launch_kv8_attention(const AttnShape& s, const AttnBatch& batch, const Kv8Pool& pool, int nchunks,
                                 const void* q, AttnPartials parts, void* out, hipStream_t stream);
+// Joins a launch's partials, whose maxima are of unscaled scores.
+hipError_t launch_kv_merge(const AttnShape& s, const AttnBatch& batch, AttnPartials parts, void* out,
+                           hipStream_t stream);
+int64_t cu_count();  // of the current device
 
 hipError_t launch_residual_norm(bool f32, int rows, int width, float eps, const void* x, const void* residual,
                                 const void* weight, void* new_residual, uint8_t* out, float* out_scale,

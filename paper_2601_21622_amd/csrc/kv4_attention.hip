@@ -1,0 +1,425 @@
+// Verification attention over a paged 4-bit cache (split-KV) for gfx950.
+//
+//   O = softmax(scale * Q K^T + mask) V,  K = code * 2^e of its key's 32 columns, V = code * s of its key.
+//
+// The G * group queries that share a KV head are the rows of one KV head.  One
+// wave, a workgroup of its own, per work item (chunk of whole 64-key blocks of one
+// request, KV head, group of rows); each item writes a partial (reference maximum, sum, O)
+// and the merge joins them in chunk order.
+//
+// A K fragment is what a lane loads: 8 codes of one key, whose scale the widening
+// instruction takes.  V lies key by key, so that an append writes rows, and is transposed on
+// its way out of LDS: a lane gets one column of the 16 keys whose scores it holds
+// (S^T = K Q^T; tile t: keys 16 t + 4 g + r of group g = lane / 16), which is all that
+// O^T += V^T P^T needs.  V's scale multiplies the weight, in float32, before the weight
+// is rounded to bfloat16 for the product with V's codes.
+//
+// Softmax in the log2 domain, against a reference that is the row's maximum as of the
+// last time it was set: scores may pass it by 2^8 before O is rescaled, which a wave
+// notices by the sums that it keeps anyway.  Accumulators start at -reference.  Where a
+// reference is so large that sums that start there round differently from those that start
+// at zero by more than a 2^8th (kCareful), and in the block that sets it, scores are summed
+// from zero and the reference is subtracted from the sum.
+#include <algorithm>
+
+#include "fp4.h"
+#include "fp8.h"
+#include "kv_wave.h"
+
+namespace sdv {
+
+namespace {
+
+constexpr int kMaxTiles4 = 64;  // blocks per chunk: one lane holds one block's page
+constexpr float kNoKey4 = -3.402823466e38f;  // reference of a row that has seen no key: no score lies below it
+constexpr float kGrow = 256.f;      // sum of a lane's 16 weights of a block that sets a new reference
+constexpr float kCareful = 65536.f;  // log2 magnitude of a reference from which sums start at zero
+
+// A wave's ring: the K and V of two blocks, codes and then scales.
+template <int D>
+struct Ring4 {
+  static constexpr int kCodes = 32 * D;
+  static constexpr int kHalf = kCodes + 256;
+  static constexpr int kOps = D / 32 + 1;  // DMAs of a half
+  static constexpr int kSlots = 4;
+};
+
+// LDS DMA of a dword a lane, as ring_dma.
+__device__ __forceinline__ void ring_dma4(const void* base, uint32_t off, uint32_t lds) {
+  uint64_t from;
+  asm volatile("s_mov_b32 m0, %1\n\ts_mov_b64 %0, %3\n\tglobal_load_lds_dword %2, %0 nt"
+               : "=&s"(from)
+               : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(off), "s"(base)
+               : "m0", "memory");
+}
+
+typedef __attribute__((__vector_size__(2 * sizeof(int)))) int i32x2;
+
+// One column of 16 keys, from the 8 bytes (16 columns of a key) that each of 16 lanes
+// points at: lane i of them gets column i, the codes in the order of the lanes.
+__device__ __forceinline__ i32x2 lds_read_tr4(const unsigned char* p) {
+  return __builtin_amdgcn_ds_read_tr4_b64_v2i32((__attribute__((address_space(3))) i32x2*)p);
+}
+
+template <int RB, int D>
+struct Wave4 {
+  bf16x8 q[RB][D / 32];
+  f32x4 o[RB][D / 16];
+  float m[RB], l[RB];  // reference of the unscaled scores (kNoKey4: no key seen yet), sum
+  uint64_t sees[RB];   // of the step's own positions
+};
+
+template <int RB, int D>
+struct Scores {
+  f32x4 s[RB][4];
+};
+
+// Scores of a block, accumulated from `base`; what a row does not see is -inf.
+template <int RB, int D, bool MASKED>
+__device__ __forceinline__ void block_scores(const Wave4<RB, D>& w, const unsigned char* kp, int off, const float (&base)[RB],
+                                             f32x4 (&sc)[RB][4]) {
+  constexpr int kSteps = D / 32;
+  const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
+  const uint32_t ks = *reinterpret_cast<const uint32_t*>(kp + Ring4<D>::kCodes + ((lg * (D / 4)) / kGroup4 * 16 + lr) * 4);
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    const float scale = __uint_as_float(((ks >> (8 * t)) & 255u) << 23);
+    uint32_t codes[kSteps];
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i)
+      codes[i] = reinterpret_cast<const uint32_t*>(kp + t * (8 * D) + lane * (D / 8))[i];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) sc[rb][t] = f32x4{base[rb], base[rb], base[rb], base[rb]};
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      const bf16x8 kf = widen8_fp4(codes[i], scale);
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) sc[rb][t] = mfma16x16x32(kf, w.q[rb][i], sc[rb][t]);
+    }
+  }
+  if (MASKED) {
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      const uint64_t win = keys_seen(w.sees[rb], off);
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const uint32_t see = (uint32_t)(win >> (16 * t + r)) & 1u;
+          const uint32_t x = __float_as_uint(sc[rb][t][r]);
+          sc[rb][t][r] = __uint_as_float(see ? x : 0xff800000u);
+        }
+    }
+  }
+}
+
+// Weights 2^(scale_log2 * difference) in place, and each row's sum over the lane's 16 keys.
+template <int RB>
+__device__ __forceinline__ void block_weights(f32x4 (&sc)[RB][4], float scale_log2, float (&sum)[RB]) {
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    float a = 0.f;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        sc[rb][t][r] = __builtin_amdgcn_exp2f(sc[rb][t][r] * scale_log2);
+        a += sc[rb][t][r];
+      }
+    sum[rb] = a;
+  }
+}
+
+template <int RB>
+__device__ __forceinline__ void less_reference(f32x4 (&sc)[RB][4], const float (&m)[RB]) {
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    const float x = m[rb] > kNoKey4 ? m[rb] : 0.f;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sc[rb][t][r] -= x;
+  }
+}
+
+template <int RB, int D>
+__global__ __launch_bounds__(kWave, 2)
+void kv4_attn_kernel(AttnShape s, AttnBatch bt, Kv4Pool pool, int nchunks, const uint16_t* __restrict__ q,
+                     AttnPartials parts) {
+  using R = Ring4<D>;
+  __shared__ __align__(1024) unsigned char ring[R::kSlots * R::kHalf];
+  const int lane = threadIdx.x & 63;
+  const int lr = lane & 15, lg = lane >> 4;
+  // Row groups of one (chunk, KV head) are 8 workgroups apart, on one XCD: the
+  // second read of a block hits its L2.
+  const int per = 8 * s.row_groups;
+  const int item = blockIdx.x / per * 8 + (blockIdx.x & 7);
+  const int rg = blockIdx.x % per >> 3;
+  if (item >= nchunks * s.Hkv) return;
+  const int head = item % s.Hkv;
+  const int c = item / s.Hkv;
+  // The largest request with chunk_prefix <= c: one load, a request per lane.
+  const int prefix = lane < bt.nreq ? bt.chunk_prefix[lane] : INT32_MAX;
+  const int lo = __popcll(__ballot(prefix <= c)) - 1;
+  const int req = bt.req0 + lo;
+  const int end = bt.kv_len[lo], first = end - s.G;
+  const int key_begin = (c - __builtin_amdgcn_readlane(prefix, lo)) * s.chunk_keys;
+  const int key_end = min(key_begin + s.chunk_keys, end);
+  const int ntiles = __builtin_amdgcn_readfirstlane((key_end - key_begin + kKeyBlock4 - 1) / kKeyBlock4);
+  const int blk0 = key_begin / kKeyBlock4;
+
+  // Lane j: where block j of the chunk lies.
+  const int shift = pool.page_shift - 6;
+  const int blk = blk0 + min(lane, ntiles - 1);
+  int page = pool.table[(int64_t)req * pool.max_pages + (blk >> shift)];
+  page = min(max(page, 0), pool.num_pages - 1);
+  const int64_t at = (((int64_t)page * s.Hkv + head) << shift) + (blk & ((1 << shift) - 1));
+  const uint32_t at_lo = (uint32_t)at, at_hi = (uint32_t)(at >> 32);
+
+  const uint32_t ring_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)ring;
+  const uint32_t off16 = lane * 16;
+  const uint32_t koff4 = (lane * 4) & (2 * D - 1), voff4 = (lane * 4) & 127;
+  // Block t's K (or V) into its place.
+  auto fetch = [&](int t, bool is_v) {
+    const int64_t b = (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)at_hi, t) << 32) |
+                                (uint32_t)__builtin_amdgcn_readlane((int)at_lo, t));
+    const uint8_t* src = (is_v ? pool.v : pool.k) + b * R::kCodes;
+    const uint32_t dst = ring_at + ((t & 1) * 2 + (is_v ? 1 : 0)) * R::kHalf;
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j) ring_dma(src + j * 1024, off16, dst + j * 1024);
+    if (is_v)
+      ring_dma4(reinterpret_cast<const uint8_t*>(pool.v_scale) + b * 128, voff4, dst + R::kCodes);
+    else
+      ring_dma4(pool.k_scale + b * (2 * D), koff4, dst + R::kCodes);
+  };
+  // A half is in once only DMAs of the `after` halves asked for after it are on their way.
+  auto wait_half = [&](int after) {
+    if (after >= 3) wait_vmcnt<3 * R::kOps>();
+    else if (after == 2) wait_vmcnt<2 * R::kOps>();
+    else if (after == 1) wait_vmcnt<R::kOps>();
+    else wait_vmcnt<0>();
+    asm volatile("" ::: "memory");
+  };
+  fetch(0, false);
+  fetch(0, true);
+  if (ntiles > 1) {
+    fetch(1, false);
+    fetch(1, true);
+  }
+
+  Wave4<RB, D> w;
+  const int whole = __builtin_amdgcn_readfirstlane(min(max((first + 1 - key_begin) / kKeyBlock4, 0), ntiles));  // blocks that every row sees whole
+  uint64_t masks = 1;  // a chunk of whole blocks ends with position 0 at the latest: all rows see it
+  if (whole < ntiles) masks = position_mask(bt.parent != nullptr ? bt.parent + (int64_t)req * (s.G - 1) : nullptr, s.G);
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    const int row = (rg * RB + rb) * 16 + lr;
+    const int rc = min(row, s.rows - 1);
+    const int j = rc / s.group, h = head * s.group + rc - j * s.group;
+    // Lane group g: the columns whose codes it holds of a key.
+    const uint16_t* src = q + (((int64_t)req * s.G + j) * s.Hq + h) * D + (D / 4) * lg;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) w.q[rb][i] = load_bf16x8(src + 8 * i);
+    const uint32_t a = __shfl((uint32_t)masks, j), b = __shfl((uint32_t)(masks >> 32), j);
+    w.sees[rb] = ((uint64_t)b << 32) | a;
+    w.m[rb] = kNoKey4;
+    w.l[rb] = 0.f;
+#pragma unroll
+    for (int db = 0; db < D / 16; ++db) w.o[rb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  bool fresh = true, careful = false;  // some row has seen no key yet; some reference is large
+  auto step = [&](int t, auto masked) {
+    constexpr bool MASKED = decltype(masked)::value;
+    const int key0 = key_begin + t * kKeyBlock4;
+    const unsigned char* kp = ring + (t & 1) * 2 * R::kHalf;
+    const unsigned char* vp = kp + R::kHalf;
+    const int left = ntiles - 1 - t;  // blocks after this one
+    wait_half(left > 0 ? 3 : 1);
+    const float c = s.scale_log2;
+    f32x4 sc[RB][4];
+    float base[RB], sum[RB];
+    const bool zero = fresh || careful;
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) base[rb] = zero ? 0.f : -w.m[rb];
+    const int off = key0 + 4 * lg - first;
+    block_scores<RB, D, MASKED>(w, kp, off, base, sc);
+    bool set = fresh;
+    if (!set) {
+      if (careful) less_reference<RB>(sc, w.m);
+      block_weights<RB>(sc, c, sum);
+      bool grow = false;
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) grow |= sum[rb] > kGrow;
+      if (__builtin_expect(__ballot(grow) != 0, 0)) {
+        set = true;
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) base[rb] = 0.f;
+        block_scores<RB, D, MASKED>(w, kp, off, base, sc);
+      }
+    }
+    if (__builtin_expect(set, 0)) {
+      bool none = false, large = false;
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        float x = kNoKey4;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          x = fmaxf(fmaxf(x, fmaxf(sc[rb][i][0], sc[rb][i][1])), fmaxf(sc[rb][i][2], sc[rb][i][3]));
+        x = fmaxf(w.m[rb], max_over_groups(x));
+        const float alpha = __builtin_amdgcn_exp2f((w.m[rb] - x) * c);
+        w.m[rb] = x;
+        w.l[rb] *= alpha;
+#pragma unroll
+        for (int db = 0; db < D / 16; ++db) w.o[rb][db] *= alpha;
+        none |= !(x > kNoKey4);
+        large |= x > kNoKey4 && fabsf(x) * c >= kCareful;
+      }
+      fresh = __ballot(none) != 0;
+      careful = __ballot(large) != 0;
+      less_reference<RB>(sc, w.m);
+      block_weights<RB>(sc, c, sum);
+    }
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) w.l[rb] += sum[rb];
+    lds_wait();  // K has been read
+    if (left > 1) fetch(t + 2, false);
+    wait_half(left > 1 ? 3 : left > 0 ? 2 : 0);
+    bf16x8 pf[RB][2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const u32x2 vs = *reinterpret_cast<const u32x2*>(vp + R::kCodes + (16 * i + 4 * lg) * 2);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float scale = __uint_as_float(r & 1 ? vs[r / 2] & 0xffff0000u : vs[r / 2] << 16);
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+          float p = sc[rb][i][r] * scale;
+          if (MASKED) {
+            // What a row does not see, and what lies past the last key, has a scale of any kind.
+            const uint32_t see = (uint32_t)(keys_seen(w.sees[rb], off) >> (16 * i + r)) & 1u;
+            p = __uint_as_float(see ? __float_as_uint(p) : 0u);
+          }
+          pf[rb][i / 2][i % 2 * 4 + r] = (__bf16)p;
+        }
+      }
+    }
+    const unsigned char* vl = vp + (16 * (lr / 4) + 4 * lg + lr % 4) * 8;
+#pragma unroll
+    for (int db = 0; db < D / 16; ++db) {
+      const i32x2 v = lds_read_tr4(vl + db * 512);
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        const bf16x8 vf = widen8_fp4((uint32_t)v[hf], 1.f);
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) w.o[rb][db] = mfma16x16x32(vf, pf[rb][hf], w.o[rb][db]);
+      }
+    }
+    lds_wait();
+    if (left > 1) fetch(t + 2, true);
+  };
+  int t = 0;
+  for (; t < whole; ++t) step(t, Kind<false>());
+  for (; t < ntiles; ++t) step(t, Kind<true>());
+
+  const int64_t slot = (int64_t)(bt.chunk_base + c) * s.Hkv + head;
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    const int row = (rg * RB + rb) * 16 + lr;
+    const float l = sum_over_groups(w.l[rb]);
+    if (row < s.rows) {
+      if (lg == 0) {
+        parts.m[slot * s.rows + row] = w.m[rb];
+        parts.l[slot * s.rows + row] = l;
+      }
+      float* dst = parts.o + (slot * s.rows + row) * D + 4 * lg;
+#pragma unroll
+      for (int db = 0; db < D / 16; ++db) *reinterpret_cast<f32x4*>(dst + db * 16) = w.o[rb][db];
+    }
+  }
+}
+
+int max_blocks4(int D) { return D == 64 ? 3 : 2; }  // 16-row blocks of a wave
+
+int blocks_of4(int rows, int groups) { return ((rows + 15) / 16 + groups - 1) / groups; }
+
+// Workgroups (one wave, one item each) that run at once: what LDS and registers hold.
+int64_t places4(int) { return cu_count() * 8; }
+
+}  // namespace
+
+AttnShape kv4_shape(int G, int Hq, int Hkv, int D, float scale, const int32_t* kv_len, int B) {
+  AttnShape s;
+  s.G = G;
+  s.Hq = Hq;
+  s.Hkv = Hkv;
+  s.D = D;
+  s.group = Hq / Hkv;
+  s.rows = G * s.group;
+  const int b = (s.rows + 15) / 16;
+  s.row_groups = (b + max_blocks4(D) - 1) / max_blocks4(D);
+  s.scale_log2 = scale * kLog2e;
+  // For a half to four rounds of items over the CUs' places the shortest chunk that
+  // fits them; of these the one that is done first, counted in keys.
+  const int64_t slots = places4(D);
+  const int64_t start = 192 + 2 * s.rows;
+  auto items = [&](int tiles) {
+    const int keys = tiles * kKeyBlock4;
+    int64_t n = 0;
+    for (int i = 0; i < B; ++i) n += (kv_len[i] + keys - 1) / keys;
+    return n * Hkv * s.row_groups;
+  };
+  const int64_t total = items(1) * kKeyBlock4;
+  int64_t best = INT64_MAX;
+  int most = kMaxTiles4;
+  s.chunk_keys = kMaxTiles4 * kKeyBlock4;
+  for (int r : {1, 2, 4, 6, 8}) {  // half rounds
+    const int64_t fit = r * slots / 2;
+    if (items(most) > fit) continue;
+    int lo = 1, hi = most;  // the shortest chunk lies in [lo, hi]
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      if (items(mid) <= fit) hi = mid; else lo = mid + 1;
+    }
+    const int64_t keys = int64_t(lo) * kKeyBlock4;
+    const int64_t n = items(lo);
+    const int64_t cost = (r <= 2 ? keys + start : (total + n * start) / slots + keys / 2) + n * s.rows * 16 / slots;
+    if (cost < best) {
+      best = cost;
+      s.chunk_keys = lo * kKeyBlock4;
+    }
+    most = lo;
+    if (lo == 1) break;
+  }
+  return s;
+}
+
+int64_t kv4_max_chunks(int Hkv, int D, int B, int64_t max_kv_len) {
+  const int64_t most = std::min(4 * places4(D) / Hkv, B * ((max_kv_len + kKeyBlock4 - 1) / kKeyBlock4));
+  const int64_t at_longest = B * ((max_kv_len + kMaxTiles4 * kKeyBlock4 - 1) / (kMaxTiles4 * kKeyBlock4));
+  return std::max(most, at_longest);
+}
+
+hipError_t launch_kv4_attention(const AttnShape& s, const AttnBatch& batch, const Kv4Pool& pool, int nchunks,
+                                const void* q, AttnPartials parts, void* out, hipStream_t stream) {
+  const dim3 grid((nchunks * s.Hkv + 7) / 8 * 8 * s.row_groups), block(kWave);
+#define SDV_KV4(RB)                                                                                               \
+  case RB:                                                                                                        \
+    if (s.D == 128 && RB <= 2)                                                                                    \
+      hipLaunchKernelGGL((kv4_attn_kernel<(RB <= 2 ? RB : 2), 128>), grid, block, 0, stream, s, batch, pool, nchunks,              \
+                         static_cast<const uint16_t*>(q), parts);                                                 \
+    else                                                                                                          \
+      hipLaunchKernelGGL((kv4_attn_kernel<RB, 64>), grid, block, 0, stream, s, batch, pool, nchunks,               \
+                         static_cast<const uint16_t*>(q), parts);                                                 \
+    break;
+  switch (blocks_of4(s.rows, s.row_groups)) {
+    SDV_KV4(1) SDV_KV4(2) SDV_KV4(3)
+    default: return hipErrorInvalidValue;
+  }
+#undef SDV_KV4
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  return launch_kv_merge(s, batch, parts, out, stream);
+}
+
+}  // namespace sdv

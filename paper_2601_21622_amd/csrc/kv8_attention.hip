@@ -48,6 +48,7 @@
 #include <atomic>
 
 #include "fp8.h"
+#include "kv_wave.h"
 
 namespace sdv {
 
@@ -72,66 +73,6 @@ struct Ring {
   static constexpr int kSlots = 5;
 };
 
-typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
-typedef __attribute__((__vector_size__(2 * sizeof(float)))) float f32x2;
-
-template <bool X>
-struct Kind {
-  static constexpr bool value = X;
-};
-template <int X>
-struct Int {
-  static constexpr int value = X;
-};
-
-// LDS DMA of 1 KB: lane l copies 16 bytes from base + off into LDS bytes lds +
-// 16 l (lds wave-uniform).  From inline assembly, so that the compiler adds no
-// waits of its own.  The base is copied by a scalar instruction first: that is the
-// wait state between the write of M0 and the load, and the load's base is never a
-// register that a vector instruction (a lane's read, a spill's) wrote just before,
-// which would take five.
-__device__ __forceinline__ void ring_dma(const void* base, uint32_t off, uint32_t lds) {
-  uint64_t from;
-  asm volatile("s_mov_b32 m0, %1\n\ts_mov_b64 %0, %3\n\tglobal_load_lds_dwordx4 %2, %0 nt"
-               : "=&s"(from)
-               : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(off), "s"(base)
-               : "m0", "memory");
-}
-
-__device__ __forceinline__ float max_over_groups(float v) {
-  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-  const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
-}
-__device__ __forceinline__ float sum_over_groups(float v) {
-  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
-  const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
-}
-
-// Positions that position `lane` (< G) sees of the step's own (bit a: position
-// a): in a chain itself and those before it, in a tree itself and its
-// ancestors, by pointer jumping over the parents.
-__device__ __forceinline__ uint64_t position_mask(const int32_t* __restrict__ parent, int G) {
-  const int lane = threadIdx.x & 63;
-  if (parent == nullptr) return lane >= 63 ? ~0ull : (2ull << lane) - 1ull;
-  int p = 0;
-  if (lane > 0 && lane < G) {
-    const int pp = parent[lane - 1];
-    p = (pp >= -1 && pp < lane - 1) ? pp + 1 : 0;
-  }
-  uint64_t m = 1ull | (1ull << lane);
-#pragma unroll
-  for (int i = 0; i < 6; ++i) {
-    const uint32_t lo = __shfl((uint32_t)m, p), hi = __shfl((uint32_t)(m >> 32), p);
-    m |= ((uint64_t)hi << 32) | lo;
-    p = __shfl(p, p);
-  }
-  return m;
-}
-
 // Bytes of a dword of four keys, the first of them `key`, that lie before `end`.
 __device__ __forceinline__ uint32_t bytes_before(int key, int end) {
   const int n = end - key;
@@ -141,15 +82,6 @@ __device__ __forceinline__ uint32_t bytes_before(int key, int end) {
 // 1 in each byte of a dword that is a NaN code.
 __device__ __forceinline__ uint32_t nan_bytes(uint32_t codes) {
   return (((codes & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7;
-}
-
-// Bit i: whether key `off` + i (counted from the first of the step's positions)
-// is seen: all keys before them, then the positions of `sees`, none after.
-__device__ __forceinline__ uint64_t keys_seen(uint64_t sees, int off) {
-  const uint64_t up = off < 64 ? sees >> (off & 63) : 0ull;
-  const int n = -off;
-  const uint64_t down = n < 64 ? (sees << (n & 63)) | ((1ull << (n & 63)) - 1ull) : ~0ull;
-  return off >= 0 ? up : down;
 }
 
 template <int RB, int D>
@@ -621,18 +553,6 @@ void kv8_merge_kernel(AttnShape s, AttnBatch bt, AttnPartials parts, uint16_t* _
   *reinterpret_cast<u32x2*>(dst) = u32x2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
 }
 
-int64_t cu_count() {
-  static std::atomic<int> cached[64];
-  int dev = 0;
-  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return 256;
-  int n = cached[dev].load(std::memory_order_relaxed);
-  if (n <= 0) {
-    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n <= 0) n = 256;
-    cached[dev].store(n, std::memory_order_relaxed);
-  }
-  return n;
-}
-
 // 16-row blocks of a wave.  One holds up to five (at head dimension 128 O takes 32
 // registers of each, Q 16); more rows are split over row groups, a wave each.  Where the
 // caches are a few blocks of keys per place, what counts is how long a wave takes for
@@ -658,6 +578,18 @@ int blocks_of(int rows, int groups) { return ((rows + 15) / 16 + groups - 1) / g
 int64_t places(int D) { return cu_count() * (D == 64 ? 8 : 4); }
 
 }  // namespace
+
+int64_t cu_count() {
+  static std::atomic<int> cached[64];
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return 256;
+  int n = cached[dev].load(std::memory_order_relaxed);
+  if (n <= 0) {
+    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n <= 0) n = 256;
+    cached[dev].store(n, std::memory_order_relaxed);
+  }
+  return n;
+}
 
 AttnShape kv8_shape(int G, int Hq, int Hkv, int D, float scale, const int32_t* kv_len, int B) {
   AttnShape s;
@@ -722,6 +654,23 @@ int64_t kv8_max_chunks(int Hkv, int D, int B, int64_t max_kv_len) {
   return std::max(most, at_longest);
 }
 
+hipError_t launch_kv_merge(const AttnShape& s, const AttnBatch& batch, AttnPartials parts, void* out,
+                           hipStream_t stream) {
+  const dim3 mgrid((s.rows * (s.D / 4) + 255) / 256, s.Hkv, batch.nreq);
+  int most = 0;
+  for (int b = 0; b < batch.nreq; ++b) most = std::max(most, batch.chunk_prefix[b + 1] - batch.chunk_prefix[b]);
+#define SDV_MERGE(DIM, MOST)                                                                                      \
+  hipLaunchKernelGGL((kv8_merge_kernel<DIM, MOST>), mgrid, dim3(256), 0, stream, s, batch, parts,                 \
+                     static_cast<uint16_t*>(out))
+  if (s.D == 128) {
+    if (most > 4) SDV_MERGE(128, 16); else SDV_MERGE(128, 4);
+  } else {
+    if (most > 4) SDV_MERGE(64, 16); else SDV_MERGE(64, 4);
+  }
+#undef SDV_MERGE
+  return hipGetLastError();
+}
+
 hipError_t launch_kv8_attention(const AttnShape& s, const AttnBatch& batch, const Kv8Pool& pool, int nchunks,
                                 const void* q, AttnPartials parts, void* out, hipStream_t stream) {
   const dim3 grid((nchunks * s.Hkv + 7) / 8 * 8 * s.row_groups), block(kWave);
@@ -741,19 +690,7 @@ hipError_t launch_kv8_attention(const AttnShape& s, const AttnBatch& batch, cons
 #undef SDV_KV8
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const dim3 mgrid((s.rows * (s.D / 4) + 255) / 256, s.Hkv, batch.nreq);
-  int most = 0;
-  for (int b = 0; b < batch.nreq; ++b) most = std::max(most, batch.chunk_prefix[b + 1] - batch.chunk_prefix[b]);
-#define SDV_MERGE(DIM, MOST)                                                                                      \
-  hipLaunchKernelGGL((kv8_merge_kernel<DIM, MOST>), mgrid, dim3(256), 0, stream, s, batch, parts,                 \
-                     static_cast<uint16_t*>(out))
-  if (s.D == 128) {
-    if (most > 4) SDV_MERGE(128, 16); else SDV_MERGE(128, 4);
-  } else {
-    if (most > 4) SDV_MERGE(64, 16); else SDV_MERGE(64, 4);
-  }
-#undef SDV_MERGE
-  return hipGetLastError();
+  return launch_kv_merge(s, batch, parts, out, stream);
 }
 
 }  // namespace sdv
