@@ -8,6 +8,7 @@ sizes, and one device for all.  A call runs on that device (and, without a
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 import re
 from typing import Sequence
@@ -17,7 +18,7 @@ import torch
 
 from . import _binding as _b
 from ._binding import SD_DTYPE_BF16, SD_DTYPE_F32, Dims
-from ._fp8 import _device, _lengths, _new_rows, _run, _typed
+from ._fp8 import _device, _lengths, _new_rows, _passes, _run, _typed
 
 SD_KV4_BLOCK = 64
 SD_KV4_GROUP = 32
@@ -112,15 +113,22 @@ def sd_kv4_workspace_bytes(dims: Dims, max_kv_len: int) -> int:
     return int(_library().sd_kv4_workspace_bytes(ctypes.byref(dims), int(max_kv_len)))
 
 
-def _head_rows(t, rows: int, dim: int, dtype, what: str):
-    """Address and row stride of [rows][heads][dim] (rows may be slices of wider ones)."""
+def _head_rows(t, shape, dtype, what: str):
+    """Address and row stride of [rows][heads][head_dim] (rows may be slices of wider ones)."""
     if t.dtype != dtype:
         raise ValueError(f"{what}: expected {dtype}, got {t.dtype}")
-    if t.dim() != 3 or t.shape[0] != rows or t.shape[2] != dim:
-        raise ValueError(f"{what}: expected rows [{rows}][heads][{dim}]")
-    if t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != dim):
+    if t.shape != shape:
+        raise ValueError(f"{what}: expected rows [{shape[0]}][{shape[1]}][{shape[2]}]")
+    row, head, column = t.stride()
+    if column != 1 or (head != shape[2] and shape[1] > 1):
         raise ValueError(f"{what}: a row must be contiguous")
-    return t.data_ptr(), t.stride(0) if rows > 1 else t.shape[1] * dim
+    return t.data_ptr(), row if shape[0] > 1 else shape[1] * shape[2]
+
+
+@functools.lru_cache(maxsize=64)
+def _rope(*fields):
+    rope = Rope(*fields)
+    return rope, ctypes.byref(rope)
 
 
 def sd_qk_norm_rope(q, k, positions, inv_freq, q_weight, k_weight, eps: float, q_out, k_out, interleaved: bool = False,
@@ -128,17 +136,19 @@ def sd_qk_norm_rope(q, k, positions, inv_freq, q_weight, k_weight, eps: float, q
     """Rows, heads and columns are q's and k's: [rows][heads][head_dim], float32 or bfloat16;
     rotary_dim is twice inv_freq's length."""
     dev = _device((q, k, positions, inv_freq, q_weight, k_weight, q_out, k_out))
-    if q.dim() != 3 or k.dim() != 3 or q.dtype not in (torch.float32, torch.bfloat16):
+    t, qh, kh = q.dtype, q.shape, k.shape
+    if len(qh) != 3 or len(kh) != 3 or (t != torch.bfloat16 and t != torch.float32):
         raise ValueError("q and k: expected float32 or bfloat16 rows [rows][heads][head_dim]")
-    rows, heads, dim = q.shape
-    t = q.dtype
-    (qp, qs), (kp, ks) = _head_rows(q, rows, dim, t, "q"), _head_rows(k, rows, dim, t, "k")
-    (qo, qos), (ko, kos) = _head_rows(q_out, rows, dim, t, "q_out"), _head_rows(k_out, rows, dim, t, "k_out")
-    if q_out.shape != q.shape or k_out.shape != k.shape:
-        raise ValueError("q_out and k_out: expected the shapes of q and k")
-    rope = Rope(rows, heads, k.shape[1], dim, 2 * inv_freq.numel(), int(bool(interleaved)),
-                SD_DTYPE_F32 if t == torch.float32 else SD_DTYPE_BF16, float(eps))
-    _run(_library().sd_qk_norm_rope, "sd_qk_norm_rope", dev, stream, ctypes.byref(rope), qp, qs, kp, ks,
+    rows, heads, dim = qh
+    if kh[0] != rows or kh[2] != dim:
+        raise ValueError(f"k: expected rows [{rows}][heads][{dim}]")
+    qp, qs = _head_rows(q, qh, t, "q")
+    kp, ks = _head_rows(k, kh, t, "k")
+    qo, qos = _head_rows(q_out, qh, t, "q_out")
+    ko, kos = _head_rows(k_out, kh, t, "k_out")
+    rope = _rope(rows, heads, kh[1], dim, 2 * inv_freq.numel(), 1 if interleaved else 0,
+                 SD_DTYPE_F32 if t == torch.float32 else SD_DTYPE_BF16, eps)[1]
+    _run(_library().sd_qk_norm_rope, "sd_qk_norm_rope", dev, stream, rope, qp, qs, kp, ks,
          _typed(positions, torch.int32, "positions", rows), _typed(inv_freq, torch.float32, "inv_freq", 0),
          None if q_weight is None else _typed(q_weight, t, "q_weight", dim),
          None if k_weight is None else _typed(k_weight, t, "k_weight", dim), qo, qos, ko, kos)
@@ -148,12 +158,13 @@ def sd_kv4_append(dims: Dims, cache: KV4Cache, k_new, v_new, new_off: Sequence[i
                   kv_len: Sequence[int], stream=None) -> None:
     dev = _device((k_new, v_new))
     cache._fits(dims, dev)
-    off, off_p = _lengths(new_off, np.int64, dims.batch, "new_off")
-    new, new_p = _lengths(new_len, np.int32, dims.batch, "new_len")
-    ln, len_p = _lengths(kv_len, np.int32, dims.batch, "kv_len")
+    B = dims.batch
+    off, off_p = _lengths(new_off, np.int64, B, "new_off")
+    new, new_p = _lengths(new_len, np.int32, B, "new_len")
+    ln, len_p = _lengths(kv_len, np.int32, B, "kv_len")
     k, k_stride = _new_rows(k_new, dims, "k_new")
     v, v_stride = _new_rows(v_new, dims, "v_new")
-    if int(((off + new) * (new > 0)).max()) > min(k_new.shape[0], v_new.shape[0]):
+    if _passes(off, new, min(k_new.shape[0], v_new.shape[0])):
         raise ValueError("new_off + new_len passes the last new row")
     if (k == 0 or v == 0) and not (new > 0).any():  # no rows at all: nothing to append
         return
@@ -166,21 +177,18 @@ def sd_kv4_read(dims: Dims, cache: KV4Cache, first: Sequence[int], count: Sequen
     """k_out and v_out: rows [T][n_kv_heads][head_dim] in dims.dtype; either may be None."""
     dev = _device((k_out, v_out))
     cache._fits(dims, dev)
-    at, at_p = _lengths(first, np.int32, dims.batch, "first")
-    n, n_p = _lengths(count, np.int32, dims.batch, "count")
-    off, off_p = _lengths(out_off, np.int64, dims.batch, "out_off")
-    last = int(((off + n) * (n > 0)).max())
-    args = []
-    for t, what in ((k_out, "k_out"), (v_out, "v_out")):
-        if t is None:
-            args += [None, 0]
-            continue
-        if last > t.shape[0]:
-            raise ValueError(f"{what}: out_off + count passes the last row")
-        args += _new_rows(t, dims, what)
-    if last == 0 and all(t is None or t.numel() == 0 for t in (k_out, v_out)):  # no rows at all: nothing to read
+    B = dims.batch
+    at, at_p = _lengths(first, np.int32, B, "first")
+    n, n_p = _lengths(count, np.int32, B, "count")
+    off, off_p = _lengths(out_off, np.int64, B, "out_off")
+    k, k_stride = (None, 0) if k_out is None else _new_rows(k_out, dims, "k_out")
+    v, v_stride = (None, 0) if v_out is None else _new_rows(v_out, dims, "v_out")
+    if _passes(off, n, min(len(t) for t in (k_out, v_out) if t is not None)):
+        raise ValueError("out_off + count passes the last row")
+    if not (k or v) and not (n > 0).any():  # no rows at all: nothing to read
         return
-    _run(_library().sd_kv4_read, "sd_kv4_read", dev, stream, ctypes.byref(dims), cache._ref, at_p, n_p, off_p, *args)
+    _run(_library().sd_kv4_read, "sd_kv4_read", dev, stream, ctypes.byref(dims), cache._ref, at_p, n_p, off_p, k, k_stride,
+         v, v_stride)
 
 
 def sd_verify_attention_kv4(dims: Dims, q, cache: KV4Cache, kv_len: Sequence[int], parent, scale: float, out, workspace,

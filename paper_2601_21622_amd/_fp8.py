@@ -116,13 +116,13 @@ def _device(tensors) -> int:
             continue
         if not isinstance(t, torch.Tensor):
             raise TypeError(f"expected a torch device tensor, got {type(t).__name__}")
-        if not t.is_cuda:
-            raise ValueError("device arguments must be GPU tensors")
         d = t.get_device()
-        if dev < 0:
+        if d != dev:
+            if d < 0:
+                raise ValueError("device arguments must be GPU tensors")
+            if dev >= 0:
+                raise ValueError("device arguments must be on one device")
             dev = d
-        elif d != dev:
-            raise ValueError("device arguments must be on one device")
     return dev
 
 
@@ -137,11 +137,23 @@ def _typed(t, dtype, what: str, elements: int) -> int:
     return t.data_ptr()
 
 
+_address, _byte = ctypes.addressof, ctypes.c_char.from_buffer
+
+
 def _lengths(a, dtype, batch: int, what: str):
     arr = np.ascontiguousarray(a, dtype=dtype)
     if arr.size != batch:
         raise ValueError(f"{what}: {arr.size} entries for {batch} requests")
-    return arr, arr.__array_interface__["data"][0]
+    try:  # a third of the other way's time
+        return arr, _address(_byte(arr))
+    except (TypeError, ValueError):  # not writable, or empty
+        return arr, arr.__array_interface__["data"][0]
+
+
+def _passes(off, count, limit: int) -> bool:
+    """Whether some request's rows end past `limit` (a request without rows has none)."""
+    end = off + count
+    return end.max() > limit and bool(((end > limit) & (count > 0)).any())
 
 
 def _run(fn, where: str, dev: int, stream, *args) -> None:
@@ -171,12 +183,13 @@ def _new_rows(t, dims: Dims, what: str):
     """Address and row stride of [T][Hkv][D] rows (rows may be slices of wider ones)."""
     if t.dtype != _TYPES.get(dims.dtype):
         raise ValueError(f"{what}: the type is not dims.dtype's")
-    if t.dim() != 3 or t.shape[1] != dims.n_kv_heads or t.shape[2] != dims.head_dim:
+    shape, heads, dim = t.shape, dims.n_kv_heads, dims.head_dim
+    if len(shape) != 3 or shape[1] != heads or shape[2] != dim:
         raise ValueError(f"{what}: expected rows [T][n_kv_heads][head_dim]")
-    if t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != dims.head_dim):
+    row, head, column = t.stride()
+    if column != 1 or (heads > 1 and head != dim):
         raise ValueError(f"{what}: a row must be contiguous")
-    row = dims.n_kv_heads * dims.head_dim
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else row
+    return t.data_ptr(), row if shape[0] > 1 else heads * dim
 
 
 def sd_kv8_append(dims: Dims, cache: KV8Cache, k_new, v_new, new_off: Sequence[int], new_len: Sequence[int],
@@ -188,7 +201,7 @@ def sd_kv8_append(dims: Dims, cache: KV8Cache, k_new, v_new, new_off: Sequence[i
     ln, len_p = _lengths(kv_len, np.int32, dims.batch, "kv_len")
     k, k_stride = _new_rows(k_new, dims, "k_new")
     v, v_stride = _new_rows(v_new, dims, "v_new")
-    if int(((off + new) * (new > 0)).max()) > min(k_new.shape[0], v_new.shape[0]):
+    if _passes(off, new, min(k_new.shape[0], v_new.shape[0])):
         raise ValueError("new_off + new_len passes the last new row")
     if k == 0 or v == 0:  # no rows at all: nothing to append
         if k_new.numel() == 0 and v_new.numel() == 0 and not (new > 0).any():

@@ -53,6 +53,14 @@ __device__ __forceinline__ void ring_dma4(const void* base, uint32_t off, uint32
                : "m0", "memory");
 }
 
+// The lane's number, counted where it is asked for: a copy held in a register would be
+// the first to be spilled, and a spill's reload waits for the DMAs before it.
+__device__ __forceinline__ uint32_t lane_here() {
+  uint32_t l;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=&v"(l));
+  return l;
+}
+
 typedef __attribute__((__vector_size__(2 * sizeof(int)))) int i32x2;
 
 // One column of 16 keys, from the 8 bytes (16 columns of a key) that each of 16 lanes
@@ -69,25 +77,20 @@ struct Wave4 {
   uint64_t sees[RB];   // of the step's own positions
 };
 
-template <int RB, int D>
-struct Scores {
-  f32x4 s[RB][4];
-};
-
-// Scores of a block, accumulated from `base`; what a row does not see is -inf.
+// Scores of half `hf` of a block (tiles 2 hf and 2 hf + 1), accumulated from `base`; what a row does not
+// see is -inf.  ks: the key's scale bytes of the four tiles.
 template <int RB, int D, bool MASKED>
-__device__ __forceinline__ void block_scores(const Wave4<RB, D>& w, const unsigned char* kp, int off, const float (&base)[RB],
-                                             f32x4 (&sc)[RB][4]) {
+__device__ __forceinline__ void half_scores4(const Wave4<RB, D>& w, const unsigned char* kp, int hf, uint32_t ks, int off,
+                                             const float (&base)[RB], f32x4 (&sc)[RB][2]) {
   constexpr int kSteps = D / 32;
-  const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
-  const uint32_t ks = *reinterpret_cast<const uint32_t*>(kp + Ring4<D>::kCodes + ((lg * (D / 4)) / kGroup4 * 16 + lr) * 4);
+  const int lane = threadIdx.x & 63;
 #pragma unroll
-  for (int t = 0; t < 4; ++t) {
-    const float scale = __uint_as_float(((ks >> (8 * t)) & 255u) << 23);
+  for (int t = 0; t < 2; ++t) {
+    const float scale = __uint_as_float(((ks >> (16 * hf + 8 * t)) & 255u) << 23);
     uint32_t codes[kSteps];
 #pragma unroll
     for (int i = 0; i < kSteps; ++i)
-      codes[i] = reinterpret_cast<const uint32_t*>(kp + t * (8 * D) + lane * (D / 8))[i];
+      codes[i] = reinterpret_cast<const uint32_t*>(kp + (2 * hf + t) * (8 * D) + lane * (D / 8))[i];
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) sc[rb][t] = f32x4{base[rb], base[rb], base[rb], base[rb]};
 #pragma unroll
@@ -100,9 +103,9 @@ __device__ __forceinline__ void block_scores(const Wave4<RB, D>& w, const unsign
   if (MASKED) {
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-      const uint64_t win = keys_seen(w.sees[rb], off);
+      const uint64_t win = keys_seen(w.sees[rb], off) >> (32 * hf);
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
+      for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const uint32_t see = (uint32_t)(win >> (16 * t + r)) & 1u;
@@ -113,51 +116,138 @@ __device__ __forceinline__ void block_scores(const Wave4<RB, D>& w, const unsign
   }
 }
 
-// Weights 2^(scale_log2 * difference) in place, and each row's sum over the lane's 16 keys.
-template <int RB>
-__device__ __forceinline__ void block_weights(f32x4 (&sc)[RB][4], float scale_log2, float (&sum)[RB]) {
+template <int D>
+__device__ __forceinline__ uint32_t key_scales4(const unsigned char* kp) {
+  const int lane = threadIdx.x & 63;
+  return *reinterpret_cast<const uint32_t*>(kp + Ring4<D>::kCodes + ((lane >> 4) * (D / 4) / kGroup4 * 16 + (lane & 15)) * 4);
+}
+
+// Sets the references that this block's scores outgrow, and rescales O and the sums.
+// Returns whether a reference is large.
+template <int RB, int D>
+__device__ __forceinline__ bool set_reference(Wave4<RB, D>& w, const unsigned char* kp, float scale_log2, int off) {
+  float zero[RB], x[RB];
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
-    float a = 0.f;
+    zero[rb] = 0.f;
+    x[rb] = kNoKey4;
+  }
+  const uint32_t ks = key_scales4<D>(kp);
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+  for (int hf = 0; hf < 2; ++hf) {
+    f32x4 sc[RB][2];
+    half_scores4<RB, D, true>(w, kp, hf, ks, off, zero, sc);
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+        x[rb] = fmaxf(fmaxf(x[rb], fmaxf(sc[rb][t][0], sc[rb][t][1])), fmaxf(sc[rb][t][2], sc[rb][t][3]));
+  }
+  bool large = false;
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    const float m = fmaxf(w.m[rb], max_over_groups(x[rb]));
+    const float alpha = __builtin_amdgcn_exp2f((w.m[rb] - m) * scale_log2);
+    w.m[rb] = m;
+    w.l[rb] *= alpha;
+#pragma unroll
+    for (int db = 0; db < D / 16; ++db) w.o[rb][db] *= alpha;
+    large |= m > kNoKey4 && fabsf(m) * scale_log2 >= kCareful;
+  }
+  return __ballot(large) != 0;
+}
+
+// Folds one block into O and the sums; false, with nothing changed, when a row's scores outgrow its
+// reference (not asked where the reference is this block's own, `own`).  MASKED serves large references
+// too (`careful`: scores are summed from zero).  refill_k asks for the block that takes K's place.
+template <int RB, int D, bool MASKED, typename RefillK>
+__device__ __forceinline__ bool fold_block4(Wave4<RB, D>& w, const unsigned char* kp, const unsigned char* vp, float scale_log2,
+                                            int off, bool own, bool careful, RefillK refill_k) {
+  const int lr = threadIdx.x & 15, lg = (threadIdx.x & 63) >> 4;
+  float base[RB], sum[RB];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    base[rb] = w.m[rb] > kNoKey4 && !(MASKED && careful) ? -w.m[rb] : 0.f;
+    sum[rb] = 0.f;
+  }
+  const uint32_t ks = key_scales4<D>(kp);
+  bf16x8 pf[RB][2];
+#pragma unroll
+  for (int hf = 0; hf < 2; ++hf) {
+    f32x4 sc[RB][2];
+    half_scores4<RB, D, MASKED>(w, kp, hf, ks, off, base, sc);
+    u32x2 vs[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) vs[t] = *reinterpret_cast<const u32x2*>(vp + Ring4<D>::kCodes + (32 * hf + 16 * t + 4 * lg) * 2);
+    if (MASKED && careful) {
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        const float m = w.m[rb] > kNoKey4 ? w.m[rb] : 0.f;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) sc[rb][t][r] -= m;
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        sc[rb][t][r] = __builtin_amdgcn_exp2f(sc[rb][t][r] * scale_log2);
-        a += sc[rb][t][r];
+        const uint32_t pair = vs[t][r / 2];
+        const float scale = __uint_as_float(r & 1 ? pair & 0xffff0000u : pair << 16);
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+          const float p = __builtin_amdgcn_exp2f(sc[rb][t][r] * scale_log2);
+          sum[rb] += p;
+          float y = p * scale;
+          if (MASKED) {
+            // What a row does not see, and what lies past the last key, has a scale of any kind.
+            const uint32_t see = (uint32_t)(keys_seen(w.sees[rb], off) >> (32 * hf + 16 * t + r)) & 1u;
+            y = __uint_as_float(see ? __float_as_uint(y) : 0u);
+          }
+          pf[rb][hf][t * 4 + r] = (__bf16)y;
+        }
       }
-    sum[rb] = a;
+    // The rounded weights are all that is kept of the scores.
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) asm volatile("" : "+v"(pf[rb][hf]));
   }
-}
-
-template <int RB>
-__device__ __forceinline__ void less_reference(f32x4 (&sc)[RB][4], const float (&m)[RB]) {
+  bool grow = false;
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
-    const float x = m[rb] > kNoKey4 ? m[rb] : 0.f;
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) sc[rb][t][r] -= x;
+    grow |= sum[rb] > kGrow;
+    // A row's first keys, whatever their weights.
+    if (MASKED) grow |= !(w.m[rb] > kNoKey4) && (keys_seen(w.sees[rb], off) & 0x000f000f000f000full) != 0;
   }
+  if (__builtin_expect(__ballot(grow) != 0 && !own, 0)) return false;
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) w.l[rb] += sum[rb];
+  lds_wait();  // K has been read
+  refill_k();
+  const unsigned char* vl = vp + (16 * (lr / 4) + 4 * lg + lr % 4) * 8;
+  i32x2 v[D / 16];
+#pragma unroll
+  for (int db = 0; db < D / 16; ++db) v[db] = lds_read_tr4(vl + db * 512);
+#pragma unroll
+  for (int db = 0; db < D / 16; ++db) {
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) {
+      const bf16x8 vf = widen8_fp4((uint32_t)v[db][hf], 1.f);
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) w.o[rb][db] = mfma16x16x32(vf, pf[rb][hf], w.o[rb][db]);
+    }
+  }
+  return true;
 }
 
+// One work item: rows from `row0` on of a chunk and KV head.
 template <int RB, int D>
-__global__ __launch_bounds__(kWave, 2)
-void kv4_attn_kernel(AttnShape s, AttnBatch bt, Kv4Pool pool, int nchunks, const uint16_t* __restrict__ q,
-                     AttnPartials parts) {
+__device__ __forceinline__ void attend_item(const AttnShape& s, const AttnBatch& bt, const Kv4Pool& pool,
+                                            const uint16_t* __restrict__ q, const AttnPartials& parts, unsigned char* ring,
+                                            int c, int head, int row0) {
   using R = Ring4<D>;
-  __shared__ __align__(1024) unsigned char ring[R::kSlots * R::kHalf];
   const int lane = threadIdx.x & 63;
   const int lr = lane & 15, lg = lane >> 4;
-  // Row groups of one (chunk, KV head) are 8 workgroups apart, on one XCD: the
-  // second read of a block hits its L2.
-  const int per = 8 * s.row_groups;
-  const int item = blockIdx.x / per * 8 + (blockIdx.x & 7);
-  const int rg = blockIdx.x % per >> 3;
-  if (item >= nchunks * s.Hkv) return;
-  const int head = item % s.Hkv;
-  const int c = item / s.Hkv;
   // The largest request with chunk_prefix <= c: one load, a request per lane.
   const int prefix = lane < bt.nreq ? bt.chunk_prefix[lane] : INT32_MAX;
   const int lo = __popcll(__ballot(prefix <= c)) - 1;
@@ -177,28 +267,19 @@ void kv4_attn_kernel(AttnShape s, AttnBatch bt, Kv4Pool pool, int nchunks, const
   const uint32_t at_lo = (uint32_t)at, at_hi = (uint32_t)(at >> 32);
 
   const uint32_t ring_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)ring;
-  const uint32_t off16 = lane * 16;
-  const uint32_t koff4 = (lane * 4) & (2 * D - 1), voff4 = (lane * 4) & 127;
   // Block t's K (or V) into its place.
   auto fetch = [&](int t, bool is_v) {
     const int64_t b = (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)at_hi, t) << 32) |
                                 (uint32_t)__builtin_amdgcn_readlane((int)at_lo, t));
     const uint8_t* src = (is_v ? pool.v : pool.k) + b * R::kCodes;
     const uint32_t dst = ring_at + ((t & 1) * 2 + (is_v ? 1 : 0)) * R::kHalf;
+    const uint32_t l = lane_here();
 #pragma unroll
-    for (int j = 0; j < D / 32; ++j) ring_dma(src + j * 1024, off16, dst + j * 1024);
+    for (int j = 0; j < D / 32; ++j) ring_dma(src + j * 1024, l * 16, dst + j * 1024);
     if (is_v)
-      ring_dma4(reinterpret_cast<const uint8_t*>(pool.v_scale) + b * 128, voff4, dst + R::kCodes);
+      ring_dma4(reinterpret_cast<const uint8_t*>(pool.v_scale) + b * 128, l * 4 & 127, dst + R::kCodes);
     else
-      ring_dma4(pool.k_scale + b * (2 * D), koff4, dst + R::kCodes);
-  };
-  // A half is in once only DMAs of the `after` halves asked for after it are on their way.
-  auto wait_half = [&](int after) {
-    if (after >= 3) wait_vmcnt<3 * R::kOps>();
-    else if (after == 2) wait_vmcnt<2 * R::kOps>();
-    else if (after == 1) wait_vmcnt<R::kOps>();
-    else wait_vmcnt<0>();
-    asm volatile("" ::: "memory");
+      ring_dma4(pool.k_scale + b * (2 * D), l * 4 & (2 * D - 1), dst + R::kCodes);
   };
   fetch(0, false);
   fetch(0, true);
@@ -213,8 +294,7 @@ void kv4_attn_kernel(AttnShape s, AttnBatch bt, Kv4Pool pool, int nchunks, const
   if (whole < ntiles) masks = position_mask(bt.parent != nullptr ? bt.parent + (int64_t)req * (s.G - 1) : nullptr, s.G);
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
-    const int row = (rg * RB + rb) * 16 + lr;
-    const int rc = min(row, s.rows - 1);
+    const int rc = min(row0 + rb * 16 + lr, s.rows - 1);
     const int j = rc / s.group, h = head * s.group + rc - j * s.group;
     // Lane group g: the columns whose codes it holds of a key.
     const uint16_t* src = q + (((int64_t)req * s.G + j) * s.Hq + h) * D + (D / 4) * lg;
@@ -228,104 +308,46 @@ void kv4_attn_kernel(AttnShape s, AttnBatch bt, Kv4Pool pool, int nchunks, const
     for (int db = 0; db < D / 16; ++db) w.o[rb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  bool fresh = true, careful = false;  // some row has seen no key yet; some reference is large
+  bool careful = false;  // some reference is large
+  int own = 0;           // the block that last set references
+  auto place = [&](int t) { return ring + (t & 1) * 2 * R::kHalf; };
+  auto offset = [&](int t) { return key_begin + t * kKeyBlock4 + 4 * lg - first; };
+  // Block t is in once only the next one's DMAs are on their way.
+  auto arrived = [&](int t) {
+    if (t + 1 < ntiles) wait_vmcnt<2 * R::kOps>();
+    else wait_vmcnt<0>();
+    asm volatile("" ::: "memory");
+  };
   auto step = [&](int t, auto masked) {
     constexpr bool MASKED = decltype(masked)::value;
-    const int key0 = key_begin + t * kKeyBlock4;
-    const unsigned char* kp = ring + (t & 1) * 2 * R::kHalf;
-    const unsigned char* vp = kp + R::kHalf;
-    const int left = ntiles - 1 - t;  // blocks after this one
-    wait_half(left > 0 ? 3 : 1);
-    const float c = s.scale_log2;
-    f32x4 sc[RB][4];
-    float base[RB], sum[RB];
-    const bool zero = fresh || careful;
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) base[rb] = zero ? 0.f : -w.m[rb];
-    const int off = key0 + 4 * lg - first;
-    block_scores<RB, D, MASKED>(w, kp, off, base, sc);
-    bool set = fresh;
-    if (!set) {
-      if (careful) less_reference<RB>(sc, w.m);
-      block_weights<RB>(sc, c, sum);
-      bool grow = false;
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) grow |= sum[rb] > kGrow;
-      if (__builtin_expect(__ballot(grow) != 0, 0)) {
-        set = true;
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) base[rb] = 0.f;
-        block_scores<RB, D, MASKED>(w, kp, off, base, sc);
-      }
+    arrived(t);
+    const unsigned char* kp = place(t);
+    const bool more = t + 2 < ntiles;
+    const bool done = fold_block4<RB, D, MASKED>(w, kp, kp + R::kHalf, s.scale_log2, offset(t), t == own, careful, [&] {
+      if (more) fetch(t + 2, false);
+    });
+    if (done) {
+      lds_wait();
+      if (more) fetch(t + 2, true);
     }
-    if (__builtin_expect(set, 0)) {
-      bool none = false, large = false;
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-        float x = kNoKey4;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          x = fmaxf(fmaxf(x, fmaxf(sc[rb][i][0], sc[rb][i][1])), fmaxf(sc[rb][i][2], sc[rb][i][3]));
-        x = fmaxf(w.m[rb], max_over_groups(x));
-        const float alpha = __builtin_amdgcn_exp2f((w.m[rb] - x) * c);
-        w.m[rb] = x;
-        w.l[rb] *= alpha;
-#pragma unroll
-        for (int db = 0; db < D / 16; ++db) w.o[rb][db] *= alpha;
-        none |= !(x > kNoKey4);
-        large |= x > kNoKey4 && fabsf(x) * c >= kCareful;
-      }
-      fresh = __ballot(none) != 0;
-      careful = __ballot(large) != 0;
-      less_reference<RB>(sc, w.m);
-      block_weights<RB>(sc, c, sum);
-    }
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) w.l[rb] += sum[rb];
-    lds_wait();  // K has been read
-    if (left > 1) fetch(t + 2, false);
-    wait_half(left > 1 ? 3 : left > 0 ? 2 : 0);
-    bf16x8 pf[RB][2];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const u32x2 vs = *reinterpret_cast<const u32x2*>(vp + R::kCodes + (16 * i + 4 * lg) * 2);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float scale = __uint_as_float(r & 1 ? vs[r / 2] & 0xffff0000u : vs[r / 2] << 16);
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-          float p = sc[rb][i][r] * scale;
-          if (MASKED) {
-            // What a row does not see, and what lies past the last key, has a scale of any kind.
-            const uint32_t see = (uint32_t)(keys_seen(w.sees[rb], off) >> (16 * i + r)) & 1u;
-            p = __uint_as_float(see ? __float_as_uint(p) : 0u);
-          }
-          pf[rb][i / 2][i % 2 * 4 + r] = (__bf16)p;
-        }
-      }
-    }
-    const unsigned char* vl = vp + (16 * (lr / 4) + 4 * lg + lr % 4) * 8;
-#pragma unroll
-    for (int db = 0; db < D / 16; ++db) {
-      const i32x2 v = lds_read_tr4(vl + db * 512);
-#pragma unroll
-      for (int hf = 0; hf < 2; ++hf) {
-        const bf16x8 vf = widen8_fp4((uint32_t)v[hf], 1.f);
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) w.o[rb][db] = mfma16x16x32(vf, pf[rb][hf], w.o[rb][db]);
-      }
-    }
-    lds_wait();
-    if (left > 1) fetch(t + 2, true);
+    return done;
   };
   int t = 0;
-  for (; t < whole; ++t) step(t, Kind<false>());
-  for (; t < ntiles; ++t) step(t, Kind<true>());
+  arrived(0);
+  for (;;) {
+    careful = set_reference<RB, D>(w, place(t), s.scale_log2, offset(t));
+    own = t;
+    bool done = true;
+    if (!careful)
+      for (; t < whole && done; t += done) done = step(__builtin_amdgcn_readfirstlane(t), Kind<false>());
+    for (; t < ntiles && done; t += done) done = step(__builtin_amdgcn_readfirstlane(t), Kind<true>());
+    if (done) break;
+  }
 
   const int64_t slot = (int64_t)(bt.chunk_base + c) * s.Hkv + head;
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
-    const int row = (rg * RB + rb) * 16 + lr;
+    const int row = row0 + rb * 16 + lr;
     const float l = sum_over_groups(w.l[rb]);
     if (row < s.rows) {
       if (lg == 0) {
@@ -339,7 +361,26 @@ void kv4_attn_kernel(AttnShape s, AttnBatch bt, Kv4Pool pool, int nchunks, const
   }
 }
 
-int max_blocks4(int D) { return D == 64 ? 3 : 2; }  // 16-row blocks of a wave
+// The first `full` row groups take RB 16-row blocks, the others one less (UNEVEN).
+template <int RB, bool UNEVEN, int D>
+__global__ __launch_bounds__(kWave, 2)
+void kv4_attn_kernel(AttnShape s, AttnBatch bt, Kv4Pool pool, int nchunks, int full, const uint16_t* __restrict__ q,
+                     AttnPartials parts) {
+  __shared__ __align__(1024) unsigned char ring[Ring4<D>::kSlots * Ring4<D>::kHalf];
+  // Row groups of one (chunk, KV head) are 8 workgroups apart, on one XCD: the
+  // second read of a block hits its L2.
+  const int per = 8 * s.row_groups;
+  const int item = blockIdx.x / per * 8 + (blockIdx.x & 7);
+  const int rg = blockIdx.x % per >> 3;
+  if (item >= nchunks * s.Hkv) return;
+  const int head = item % s.Hkv, c = item / s.Hkv;
+  if (!UNEVEN || rg < full)
+    attend_item<RB, D>(s, bt, pool, q, parts, ring, c, head, rg * RB * 16);
+  else
+    attend_item<(UNEVEN ? RB - 1 : RB), D>(s, bt, pool, q, parts, ring, c, head, (rg * (RB - 1) + full) * 16);
+}
+
+int max_blocks4(int) { return 3; }  // 16-row blocks of a wave
 
 int blocks_of4(int rows, int groups) { return ((rows + 15) / 16 + groups - 1) / groups; }
 
@@ -403,19 +444,22 @@ int64_t kv4_max_chunks(int Hkv, int D, int B, int64_t max_kv_len) {
 hipError_t launch_kv4_attention(const AttnShape& s, const AttnBatch& batch, const Kv4Pool& pool, int nchunks,
                                 const void* q, AttnPartials parts, void* out, hipStream_t stream) {
   const dim3 grid((nchunks * s.Hkv + 7) / 8 * 8 * s.row_groups), block(kWave);
-#define SDV_KV4(RB)                                                                                               \
-  case RB:                                                                                                        \
-    if (s.D == 128 && RB <= 2)                                                                                    \
-      hipLaunchKernelGGL((kv4_attn_kernel<(RB <= 2 ? RB : 2), 128>), grid, block, 0, stream, s, batch, pool, nchunks,              \
+  const int blocks = (s.rows + 15) / 16, most = blocks_of4(s.rows, s.row_groups);
+  const int full = blocks - (most - 1) * s.row_groups;  // row groups of `most` blocks
+#define SDV_KV4(RB, UNEVEN)                                                                                       \
+  do {                                                                                                            \
+    if (s.D == 128)                                                                                               \
+      hipLaunchKernelGGL((kv4_attn_kernel<RB, UNEVEN, 128>), grid, block, 0, stream, s, batch, pool, nchunks, full, \
                          static_cast<const uint16_t*>(q), parts);                                                 \
     else                                                                                                          \
-      hipLaunchKernelGGL((kv4_attn_kernel<RB, 64>), grid, block, 0, stream, s, batch, pool, nchunks,               \
+      hipLaunchKernelGGL((kv4_attn_kernel<RB, UNEVEN, 64>), grid, block, 0, stream, s, batch, pool, nchunks, full, \
                          static_cast<const uint16_t*>(q), parts);                                                 \
-    break;
-  switch (blocks_of4(s.rows, s.row_groups)) {
-    SDV_KV4(1) SDV_KV4(2) SDV_KV4(3)
-    default: return hipErrorInvalidValue;
-  }
+  } while (0)
+  if (most == 1) SDV_KV4(1, false);
+  else if (most == 2 && full == s.row_groups) SDV_KV4(2, false);
+  else if (most == 2) SDV_KV4(2, true);
+  else if (full == s.row_groups) SDV_KV4(3, false);
+  else SDV_KV4(3, true);
 #undef SDV_KV4
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
