@@ -44,12 +44,31 @@ struct Ring4 {
   static constexpr int kSlots = 4;
 };
 
-// LDS DMA of a dword a lane, as ring_dma.
-__device__ __forceinline__ void ring_dma4(const void* base, uint32_t off, uint32_t lds) {
+// The DMAs of a half: D / 32 KB of codes, 16 bytes a lane each, then a dword a lane of
+// scales, whose base and offset are their own.  As ring_dma, with one base for the codes: a
+// DMA's offset is added on both sides.
+template <int D>
+__device__ __forceinline__ void half_dma(const void* codes, uint32_t off16, uint32_t lds, const void* scales, uint32_t off4,
+                                         uint32_t lds_scales) {
   uint64_t from;
+  if (D == 128)
+    asm volatile(
+        "s_mov_b32 m0, %1\n\ts_mov_b64 %0, %3\n\tglobal_load_lds_dwordx4 %2, %0 nt\n\t"
+        "global_load_lds_dwordx4 %2, %0 offset:1024 nt\n\tglobal_load_lds_dwordx4 %2, %0 offset:2048 nt\n\t"
+        "global_load_lds_dwordx4 %2, %0 offset:3072 nt"
+        : "=&s"(from)
+        : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(off16), "s"(codes)
+        : "m0", "memory");
+  else
+    asm volatile(
+        "s_mov_b32 m0, %1\n\ts_mov_b64 %0, %3\n\tglobal_load_lds_dwordx4 %2, %0 nt\n\t"
+        "global_load_lds_dwordx4 %2, %0 offset:1024 nt"
+        : "=&s"(from)
+        : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(off16), "s"(codes)
+        : "m0", "memory");
   asm volatile("s_mov_b32 m0, %1\n\ts_mov_b64 %0, %3\n\tglobal_load_lds_dword %2, %0 nt"
                : "=&s"(from)
-               : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(off), "s"(base)
+               : "s"(__builtin_amdgcn_readfirstlane(lds_scales)), "v"(off4), "s"(scales)
                : "m0", "memory");
 }
 
@@ -77,28 +96,46 @@ struct Wave4 {
   uint64_t sees[RB];   // of the step's own positions
 };
 
+// The instructions since the last call as M products with at most V vector
+// instructions among them, one product first, so that the vector ones issue
+// while the matrix core works.
+template <int M, int V>
+__device__ __forceinline__ void interleave4() {
+#pragma unroll
+  for (int i = 0; i < M; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x002, (V + M - 1) / M, 0);
+  }
+  __builtin_amdgcn_sched_barrier(0);
+}
+
 // Scores of half `hf` of a block (tiles 2 hf and 2 hf + 1), accumulated from `base`; what a row does not
 // see is -inf.  ks: the key's scale bytes of the four tiles.
 template <int RB, int D, bool MASKED>
 __device__ __forceinline__ void half_scores4(const Wave4<RB, D>& w, const unsigned char* kp, int hf, uint32_t ks, int off,
                                              const float (&base)[RB], f32x4 (&sc)[RB][2]) {
-  constexpr int kSteps = D / 32;
-  const int lane = threadIdx.x & 63;
+  constexpr int kSteps = D / 32;  // 32-wide steps of a score tile
+  const int lane = lane_here();
+  uint32_t codes[2 * kSteps];
+  float scale[2];
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
-    const float scale = __uint_as_float(((ks >> (16 * hf + 8 * t)) & 255u) << 23);
-    uint32_t codes[kSteps];
+    scale[t] = __uint_as_float(((ks >> (16 * hf + 8 * t)) & 255u) << 23);
 #pragma unroll
     for (int i = 0; i < kSteps; ++i)
-      codes[i] = reinterpret_cast<const uint32_t*>(kp + (2 * hf + t) * (8 * D) + lane * (D / 8))[i];
+      codes[t * kSteps + i] = reinterpret_cast<const uint32_t*>(kp + (2 * hf + t) * (8 * D) + lane * (D / 8))[i];
+  }
+  bf16x8 kf = widen8_fp4(codes[0], scale[0]);
+  // The two tiles in turn: a product's sum is not asked for by the next RB * 2 - 1.
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) sc[rb][t] = f32x4{base[rb], base[rb], base[rb], base[rb]};
+  for (int n = 0; n < 2 * kSteps; ++n) {
+    const int t = n % 2, i = n / 2;
+    const bf16x8 now = kf;
+    if (n + 1 < 2 * kSteps) kf = widen8_fp4(codes[(n + 1) % 2 * kSteps + (n + 1) / 2], scale[(n + 1) % 2]);  // under this step's products
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i) {
-      const bf16x8 kf = widen8_fp4(codes[i], scale);
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) sc[rb][t] = mfma16x16x32(kf, w.q[rb][i], sc[rb][t]);
-    }
+    for (int rb = 0; rb < RB; ++rb)
+      sc[rb][t] = mfma16x16x32(now, w.q[rb][i], i == 0 ? f32x4{base[rb], base[rb], base[rb], base[rb]} : sc[rb][t]);
+    interleave4<RB, 4>();
   }
   if (MASKED) {
 #pragma unroll
@@ -118,7 +155,7 @@ __device__ __forceinline__ void half_scores4(const Wave4<RB, D>& w, const unsign
 
 template <int D>
 __device__ __forceinline__ uint32_t key_scales4(const unsigned char* kp) {
-  const int lane = threadIdx.x & 63;
+  const int lane = lane_here();
   return *reinterpret_cast<const uint32_t*>(kp + Ring4<D>::kCodes + ((lane >> 4) * (D / 4) / kGroup4 * 16 + (lane & 15)) * 4);
 }
 
@@ -163,7 +200,6 @@ __device__ __forceinline__ bool set_reference(Wave4<RB, D>& w, const unsigned ch
 template <int RB, int D, bool MASKED, typename RefillK>
 __device__ __forceinline__ bool fold_block4(Wave4<RB, D>& w, const unsigned char* kp, const unsigned char* vp, float scale_log2,
                                             int off, bool own, bool careful, RefillK refill_k) {
-  const int lr = threadIdx.x & 15, lg = (threadIdx.x & 63) >> 4;
   float base[RB], sum[RB];
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
@@ -176,6 +212,7 @@ __device__ __forceinline__ bool fold_block4(Wave4<RB, D>& w, const unsigned char
   for (int hf = 0; hf < 2; ++hf) {
     f32x4 sc[RB][2];
     half_scores4<RB, D, MASKED>(w, kp, hf, ks, off, base, sc);
+    const int lg = lane_here() >> 4;
     u32x2 vs[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) vs[t] = *reinterpret_cast<const u32x2*>(vp + Ring4<D>::kCodes + (32 * hf + 16 * t + 4 * lg) * 2);
@@ -224,18 +261,20 @@ __device__ __forceinline__ bool fold_block4(Wave4<RB, D>& w, const unsigned char
   for (int rb = 0; rb < RB; ++rb) w.l[rb] += sum[rb];
   lds_wait();  // K has been read
   refill_k();
+  const int lane = lane_here(), lr = lane & 15, lg = lane >> 4;
   const unsigned char* vl = vp + (16 * (lr / 4) + 4 * lg + lr % 4) * 8;
   i32x2 v[D / 16];
 #pragma unroll
   for (int db = 0; db < D / 16; ++db) v[db] = lds_read_tr4(vl + db * 512);
+  bf16x8 vf = widen8_fp4((uint32_t)v[0][0], 1.f);
 #pragma unroll
-  for (int db = 0; db < D / 16; ++db) {
+  for (int n = 0; n < D / 8; ++n) {
+    const int db = n % (D / 16), hf = n / (D / 16);
+    const bf16x8 now = vf;
+    if (n + 1 < D / 8) vf = widen8_fp4((uint32_t)v[(n + 1) % (D / 16)][(n + 1) / (D / 16)], 1.f);  // under this fragment's products
 #pragma unroll
-    for (int hf = 0; hf < 2; ++hf) {
-      const bf16x8 vf = widen8_fp4((uint32_t)v[db][hf], 1.f);
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) w.o[rb][db] = mfma16x16x32(vf, pf[rb][hf], w.o[rb][db]);
-    }
+    for (int rb = 0; rb < RB; ++rb) w.o[rb][db] = mfma16x16x32(now, pf[rb][hf], w.o[rb][db]);
+    interleave4<RB, 4>();
   }
   return true;
 }
@@ -274,12 +313,9 @@ __device__ __forceinline__ void attend_item(const AttnShape& s, const AttnBatch&
     const uint8_t* src = (is_v ? pool.v : pool.k) + b * R::kCodes;
     const uint32_t dst = ring_at + ((t & 1) * 2 + (is_v ? 1 : 0)) * R::kHalf;
     const uint32_t l = lane_here();
-#pragma unroll
-    for (int j = 0; j < D / 32; ++j) ring_dma(src + j * 1024, l * 16, dst + j * 1024);
-    if (is_v)
-      ring_dma4(reinterpret_cast<const uint8_t*>(pool.v_scale) + b * 128, l * 4 & 127, dst + R::kCodes);
-    else
-      ring_dma4(pool.k_scale + b * (2 * D), l * 4 & (2 * D - 1), dst + R::kCodes);
+    half_dma<D>(src, l * 16, dst,
+                is_v ? reinterpret_cast<const uint8_t*>(pool.v_scale) + b * 128 : pool.k_scale + b * (2 * D),
+                l * 4 & (is_v ? 127 : 2 * D - 1), dst + R::kCodes);
   };
   fetch(0, false);
   fetch(0, true);
@@ -311,7 +347,7 @@ __device__ __forceinline__ void attend_item(const AttnShape& s, const AttnBatch&
   bool careful = false;  // some reference is large
   int own = 0;           // the block that last set references
   auto place = [&](int t) { return ring + (t & 1) * 2 * R::kHalf; };
-  auto offset = [&](int t) { return key_begin + t * kKeyBlock4 + 4 * lg - first; };
+  auto offset = [&](int t) { return key_begin + t * kKeyBlock4 + 4 * ((int)lane_here() >> 4) - first; };
   // Block t is in once only the next one's DMAs are on their way.
   auto arrived = [&](int t) {
     if (t + 1 < ntiles) wait_vmcnt<2 * R::kOps>();

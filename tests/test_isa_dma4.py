@@ -1,5 +1,6 @@
 """LDS DMAs of the 4-bit attention, in the built gfx950 code: each takes its base from
-registers that the scalar instruction right before it wrote."""
+registers that the scalar instruction right before it, or before the DMAs of the same
+base right before it, wrote."""
 
 import glob
 import os
@@ -12,7 +13,32 @@ import pytest
 import paper_2601_21622_amd as sd
 from paper_2601_21622_amd import build as sd_build
 
-from test_isa_dma import OBJDUMP, unguarded
+from test_isa_dma import OBJDUMP
+
+
+def unguarded(lines):
+    """(DMAs seen, those whose base no instruction before the run of DMAs copies)."""
+    seen, found, base = 0, [], None
+    for line in lines:
+        text = line.split("//")[0].strip()
+        if not text or text.endswith(":"):
+            continue
+        copy = re.match(r"s_mov_b64 (s\[\d+:\d+\]),", text)
+        m = re.match(r"global_load_lds_\w+ v\d+, (s\[\d+:\d+\])", text)
+        if text.startswith("global_load_lds"):
+            seen += 1
+            if m is None or m[1] != base:
+                found.append(text)
+        else:
+            base = copy and copy[1]
+    return seen, found
+
+
+def test_the_scan_sees_an_unguarded_load():
+    copy, load, more = "\ts_mov_b64 s[4:5], s[8:9]", "\tglobal_load_lds_dwordx4 v54, s[4:5] nt", "\tglobal_load_lds_dwordx4 v54, s[4:5] offset:1024 nt"
+    assert unguarded([copy, load, more]) == (2, [])
+    assert len(unguarded([copy, load, "\ts_nop 0", more])[1]) == 1
+    assert len(unguarded([copy, "\tv_readlane_b32 s4, v1, 0", load, more])[1]) == 2
 
 
 @pytest.mark.skipif(not os.path.exists(OBJDUMP), reason="no llvm-objdump")
