@@ -13,6 +13,7 @@ namespace sdv {
 
 constexpr int kKeyBlock4 = 64;  // keys of a block
 constexpr int kGroup4 = 32;     // columns of a key's scale
+constexpr int kTile = 16;       // keys of a tile: a score tile of the attention, a wave's work elsewhere
 
 struct Kv4Pool {
   uint8_t* k;
@@ -24,8 +25,8 @@ struct Kv4Pool {
 };
 
 // Requests of one append or read launch: keys first .. first + count - 1 are rows off .. .
-// A wave takes keys_per_wave(D) keys, the first of them a multiple of that;
-// `prefix` counts the waves that a request takes.
+// A wave takes a tile of 16 keys, the first of them a multiple of 16; `prefix` counts the
+// tiles that a request takes.
 struct Kv4Rows {
   int32_t nreq;
   int32_t req[kMaxReqPerLaunch];  // rows of the block table
@@ -34,7 +35,6 @@ struct Kv4Rows {
   int32_t count[kMaxReqPerLaunch];
   int64_t off[kMaxReqPerLaunch];
 };
-constexpr int kv4_keys_per_wave(int D) { return kWave * 8 / D; }
 hipError_t launch_kv4_append(const Kv4Rows& r, const Kv4Pool& pool, int Hkv, int D, bool f32, const void* k_new,
                              int64_t k_stride, const void* v_new, int64_t v_stride, hipStream_t stream);
 hipError_t launch_kv4_read(const Kv4Rows& r, const Kv4Pool& pool, int Hkv, int D, bool f32, void* k_out,

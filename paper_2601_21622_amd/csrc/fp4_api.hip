@@ -52,8 +52,7 @@ bool rows_ok(const sd_dims_t* d, const void* p, int64_t stride) {
 // launch as its table and its grid hold.
 template <typename Launch>
 int over_rows(const sd_dims_t* d, const int32_t* first, const int32_t* count, const int64_t* off, Launch launch) {
-  const int kKeys = kv4_keys_per_wave(d->head_dim);
-  const int64_t most = kMaxGrid * 4 / (2 * int64_t(d->n_kv_heads));  // waves per head, four to a workgroup
+  const int64_t most = kMaxGrid * 4 / d->n_kv_heads;  // tiles of a launch: a wave for each and head, four to a workgroup
   Kv4Rows r;
   memset(&r, 0, sizeof(r));
   for (int b = 0; b < d->batch; ++b) {
@@ -63,13 +62,13 @@ int over_rows(const sd_dims_t* d, const int32_t* first, const int32_t* count, co
         if (launch(r) != hipSuccess) return SD_ERR_HIP;
         r.nreq = 0;
       }
-      const int64_t waves = std::min((end + kKeys - 1) / kKeys - at / kKeys, most - r.prefix[r.nreq]);
-      const int64_t stop = std::min(end, (at / kKeys + waves) * kKeys);
+      const int64_t tiles = std::min((end + kTile - 1) / kTile - at / kTile, most - r.prefix[r.nreq]);
+      const int64_t stop = std::min(end, (at / kTile + tiles) * kTile);
       r.req[r.nreq] = b;
       r.first[r.nreq] = static_cast<int32_t>(at);
       r.count[r.nreq] = static_cast<int32_t>(stop - at);
       r.off[r.nreq] = row;
-      r.prefix[r.nreq + 1] = static_cast<int32_t>(r.prefix[r.nreq] + waves);
+      r.prefix[r.nreq + 1] = static_cast<int32_t>(r.prefix[r.nreq] + tiles);
       ++r.nreq;
       row += stop - at;
       at = stop;

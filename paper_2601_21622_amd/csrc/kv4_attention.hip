@@ -41,7 +41,6 @@ struct Ring4 {
   static constexpr int kCodes = 32 * D;
   static constexpr int kHalf = kCodes + 256;
   static constexpr int kOps = D / 32 + 1;  // DMAs of a half
-  static constexpr int kSlots = 4;
 };
 
 // The DMAs of a half: D / 32 KB of codes, 16 bytes a lane each, then a dword a lane of
@@ -279,8 +278,8 @@ __device__ __forceinline__ bool fold_block4(Wave4<RB, D>& w, const unsigned char
   return true;
 }
 
-// One work item: rows from `row0` on of a chunk and KV head.
-template <int RB, int D>
+// One work item: rows from `row0` on of a chunk and KV head; a ring of N blocks.
+template <int RB, int D, int N>
 __device__ __forceinline__ void attend_item(const AttnShape& s, const AttnBatch& bt, const Kv4Pool& pool,
                                             const uint16_t* __restrict__ q, const AttnPartials& parts, unsigned char* ring,
                                             int c, int head, int row0) {
@@ -311,18 +310,18 @@ __device__ __forceinline__ void attend_item(const AttnShape& s, const AttnBatch&
     const int64_t b = (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)at_hi, t) << 32) |
                                 (uint32_t)__builtin_amdgcn_readlane((int)at_lo, t));
     const uint8_t* src = (is_v ? pool.v : pool.k) + b * R::kCodes;
-    const uint32_t dst = ring_at + ((t & 1) * 2 + (is_v ? 1 : 0)) * R::kHalf;
+    const uint32_t dst = ring_at + (t % N * 2 + (is_v ? 1 : 0)) * R::kHalf;
     const uint32_t l = lane_here();
     half_dma<D>(src, l * 16, dst,
                 is_v ? reinterpret_cast<const uint8_t*>(pool.v_scale) + b * 128 : pool.k_scale + b * (2 * D),
                 l * 4 & (is_v ? 127 : 2 * D - 1), dst + R::kCodes);
   };
-  fetch(0, false);
-  fetch(0, true);
-  if (ntiles > 1) {
-    fetch(1, false);
-    fetch(1, true);
-  }
+#pragma unroll
+  for (int t = 0; t < N; ++t)
+    if (t < ntiles) {
+      fetch(t, false);
+      fetch(t, true);
+    }
 
   Wave4<RB, D> w;
   const int whole = __builtin_amdgcn_readfirstlane(min(max((first + 1 - key_begin) / kKeyBlock4, 0), ntiles));  // blocks that every row sees whole
@@ -346,11 +345,15 @@ __device__ __forceinline__ void attend_item(const AttnShape& s, const AttnBatch&
 
   bool careful = false;  // some reference is large
   int own = 0;           // the block that last set references
-  auto place = [&](int t) { return ring + (t & 1) * 2 * R::kHalf; };
+  auto place = [&](int t) { return ring + t % N * 2 * R::kHalf; };
   auto offset = [&](int t) { return key_begin + t * kKeyBlock4 + 4 * ((int)lane_here() >> 4) - first; };
-  // Block t is in once only the next one's DMAs are on their way.
+  // Block t is in once only the next N - 1 blocks' DMAs are on their way.
   auto arrived = [&](int t) {
-    if (t + 1 < ntiles) wait_vmcnt<2 * R::kOps>();
+    static_assert((N - 1) * 2 * R::kOps < 64 && N <= 4, "vmcnt holds 6 bits");
+    const int after = min(ntiles - 1 - t, N - 1);
+    if (N > 3 && after == 3) wait_vmcnt<6 * R::kOps>();
+    else if (N > 2 && after == 2) wait_vmcnt<4 * R::kOps>();
+    else if (after >= 1) wait_vmcnt<2 * R::kOps>();
     else wait_vmcnt<0>();
     asm volatile("" ::: "memory");
   };
@@ -358,13 +361,13 @@ __device__ __forceinline__ void attend_item(const AttnShape& s, const AttnBatch&
     constexpr bool MASKED = decltype(masked)::value;
     arrived(t);
     const unsigned char* kp = place(t);
-    const bool more = t + 2 < ntiles;
+    const bool more = t + N < ntiles;
     const bool done = fold_block4<RB, D, MASKED>(w, kp, kp + R::kHalf, s.scale_log2, offset(t), t == own, careful, [&] {
-      if (more) fetch(t + 2, false);
+      if (more) fetch(t + N, false);
     });
     if (done) {
       lds_wait();
-      if (more) fetch(t + 2, true);
+      if (more) fetch(t + N, true);
     }
     return done;
   };
@@ -399,10 +402,11 @@ __device__ __forceinline__ void attend_item(const AttnShape& s, const AttnBatch&
 
 // The first `full` row groups take RB 16-row blocks, the others one less (UNEVEN).
 template <int RB, bool UNEVEN, int D>
-__global__ __launch_bounds__(kWave, 2)
+__global__ __launch_bounds__(kWave, RB > 3 ? 1 : 2)
 void kv4_attn_kernel(AttnShape s, AttnBatch bt, Kv4Pool pool, int nchunks, int full, const uint16_t* __restrict__ q,
                      AttnPartials parts) {
-  __shared__ __align__(1024) unsigned char ring[Ring4<D>::kSlots * Ring4<D>::kHalf];
+  constexpr int N = RB > 3 ? 4 : 2;
+  __shared__ __align__(1024) unsigned char ring[2 * N * Ring4<D>::kHalf];
   // Row groups of one (chunk, KV head) are 8 workgroups apart, on one XCD: the
   // second read of a block hits its L2.
   const int per = 8 * s.row_groups;
@@ -411,12 +415,12 @@ void kv4_attn_kernel(AttnShape s, AttnBatch bt, Kv4Pool pool, int nchunks, int f
   if (item >= nchunks * s.Hkv) return;
   const int head = item % s.Hkv, c = item / s.Hkv;
   if (!UNEVEN || rg < full)
-    attend_item<RB, D>(s, bt, pool, q, parts, ring, c, head, rg * RB * 16);
+    attend_item<RB, D, N>(s, bt, pool, q, parts, ring, c, head, rg * RB * 16);
   else
-    attend_item<(UNEVEN ? RB - 1 : RB), D>(s, bt, pool, q, parts, ring, c, head, (rg * (RB - 1) + full) * 16);
+    attend_item<(UNEVEN ? RB - 1 : RB), D, N>(s, bt, pool, q, parts, ring, c, head, (rg * (RB - 1) + full) * 16);
 }
 
-int max_blocks4(int) { return 3; }  // 16-row blocks of a wave
+int max_blocks4(int) { return 5; }  // 16-row blocks of a wave
 
 int blocks_of4(int rows, int groups) { return ((rows + 15) / 16 + groups - 1) / groups; }
 
@@ -494,8 +498,10 @@ hipError_t launch_kv4_attention(const AttnShape& s, const AttnBatch& batch, cons
   if (most == 1) SDV_KV4(1, false);
   else if (most == 2 && full == s.row_groups) SDV_KV4(2, false);
   else if (most == 2) SDV_KV4(2, true);
-  else if (full == s.row_groups) SDV_KV4(3, false);
-  else SDV_KV4(3, true);
+  else if (most == 3 && full == s.row_groups) SDV_KV4(3, false);
+  else if (most == 3) SDV_KV4(3, true);
+  else if (most == 4) SDV_KV4(4, false);
+  else SDV_KV4(5, false);
 #undef SDV_KV4
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;

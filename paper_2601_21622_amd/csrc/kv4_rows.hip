@@ -1,9 +1,11 @@
 // Appending key and value rows to a paged 4-bit cache, and reading them back (gfx950).
 //
 // No scale spans keys, so a key is its own unit and nothing in the cache is read
-// when one is written.  A thread holds eight columns of one key: the 32 columns of a
-// key's scale are four threads, a value's row D / 8, and eight codes are one dword.
-#include <algorithm>
+// when one is written.  A wave takes 16 keys of a block (a tile) and one KV head, K and V
+// both: D / 8 threads hold a row of eight columns each, so that rows are read and written
+// whole; on the cache's side a tile of K is 16 D / 2 bytes in a row and a tile of V 128 bytes
+// in each of the D / 16 column groups, and the two orders meet in LDS.
+#include <type_traits>
 
 #include "fp4.h"
 
@@ -15,54 +17,43 @@ constexpr int kRowThreads = 256;
 constexpr int kLowestExp4 = 27;  // byte of the smallest scale, 2^-100
 constexpr uint32_t kInfBits = 0x7f800000u;
 
-// One thread's eight columns of one key.
-template <int D>
-struct Place {
-  bool is_v, mine;  // mine: the key is one of the request's
-  int head, col;
-  int key;          // of its block
-  int64_t block;    // of the pool: [page][head][block]
-  int64_t row;      // of the rows
+// A wave's tile.
+struct Tile {
+  int head;
+  int key0;       // of its block: 0, 16, 32 or 48
+  int from, to;   // keys key0 + from .. key0 + to - 1 are the request's
+  int64_t block;  // of the pool: [page][head][block]
+  int64_t row0;   // row of key0
 };
 
-template <int D>
-__device__ __forceinline__ Place<D> place_of(const Kv4Rows& r, const Kv4Pool& pool, int Hkv, int unit) {
-  constexpr int TPR = D / 8;
-  constexpr int kKeys = kv4_keys_per_wave(D);
+__device__ __forceinline__ Tile tile_of(const Kv4Rows& r, const Kv4Pool& pool, int Hkv, int unit) {
   const int lane = threadIdx.x & 63;
-  const int waves = r.prefix[r.nreq];
-  const int c = unit % waves, hv = unit / waves;
+  Tile t;
+  t.head = unit % Hkv;
+  const int c = unit / Hkv;
   // The largest request with prefix <= c: one load, a request per lane.
   const int prefix = lane < r.nreq ? r.prefix[lane] : INT32_MAX;
   const int lo = __popcll(__ballot(prefix <= c)) - 1;
   const int first = r.first[lo], end = first + r.count[lo];
-  const int key0 = (first / kKeys + c - __builtin_amdgcn_readlane(prefix, lo)) * kKeys;
-  Place<D> p;
-  p.is_v = hv >= Hkv;
-  p.head = p.is_v ? hv - Hkv : hv;
-  p.col = lane % TPR * 8;
-  const int key = key0 + lane / TPR;
-  p.mine = key >= first && key < end;
-  const int at = min(max(key, first), end - 1);  // a key of the request's is read in its place
-  p.row = r.off[lo] + (at - first);
-  const int shift = pool.page_shift - 6, blk = at / kKeyBlock4;
+  const int key = (first / kTile + c - __builtin_amdgcn_readlane(prefix, lo)) * kTile;
+  t.from = __builtin_amdgcn_readfirstlane(max(first - key, 0));
+  t.to = __builtin_amdgcn_readfirstlane(min(end - key, kTile));
+  t.row0 = r.off[lo] + (key - first);
+  const int shift = pool.page_shift - 6, blk = key / kKeyBlock4;
   int page = pool.table[(int64_t)r.req[lo] * pool.max_pages + (blk >> shift)];
   page = min(max(page, 0), pool.num_pages - 1);
-  p.block = (((int64_t)page * Hkv + p.head) << shift) + (blk & ((1 << shift) - 1));
-  p.key = at % kKeyBlock4;
-  return p;
+  t.block = (((int64_t)page * Hkv + t.head) << shift) + (blk & ((1 << shift) - 1));
+  t.key0 = key % kKeyBlock4;
+  return t;
 }
 
-// Where the dword of the codes of columns col .. + 7 of a key lies in its block.
+// Where the dword of the codes of columns col .. + 7 of a tile's key lies among the tile's.
 template <int D>
-__device__ __forceinline__ int k_dword(int key, int col) {  // [4 t][4 g][16 r][D/8 bytes]
-  return (((key / 16 * 4 + col / (D / 4)) * 16 + key % 16) * (D / 8) + col % (D / 4) / 2) / 4;
+__device__ __forceinline__ int k_dword(int key, int col) {  // [4 g][16 r][D/8 bytes]
+  return ((col / (D / 4) * 16 + key) * (D / 8) + col % (D / 4) / 2) / 4;
 }
-__device__ __forceinline__ int v_dword(int key, int col) {  // [D/16][64 n][8 bytes]
-  return (col / 16 * 64 + key) * 2 + col % 16 / 8;
-}
-__device__ __forceinline__ int k_scale_byte(int key, int col) {  // [D/32][16 r][4 t]
-  return (col / kGroup4 * 16 + key % 16) * 4 + key / 16;
+__device__ __forceinline__ int v_dword(int key, int col) {  // [D/16][16 n][8 bytes]
+  return (col / 16 * kTile + key) * 2 + col % 16 / 8;
 }
 
 // Largest over the four threads of a key's scale.
@@ -111,35 +102,78 @@ template <typename T, int D>
 __global__ __launch_bounds__(kRowThreads)
 void kv4_append_kernel(Kv4Rows rows, Kv4Pool pool, int Hkv, int nunits, const T* __restrict__ k_new,
                        int64_t k_stride, const T* __restrict__ v_new, int64_t v_stride) {
-  const int unit = blockIdx.x * (kRowThreads / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  constexpr int TPR = D / 8, kKeys = kWave / TPR;  // threads of a row, keys at once
+  constexpr int kRounds = kTile / kKeys;
+  constexpr int kWords = kTile * D / 8;            // dwords of a tile of K, or of V
+  __shared__ __align__(16) uint32_t image[kRowThreads / kWave][2 * kWords];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int unit = blockIdx.x * (kRowThreads / kWave) + wave;
   if (unit >= nunits) return;
-  const Place<D> p = place_of<D>(rows, pool, Hkv, unit);
-  float x[8];
-  load_row8((p.is_v ? v_new + p.row * v_stride : k_new + p.row * k_stride) + p.head * D + p.col, x);
-  uint32_t most = 0;  // of the magnitudes' bits, whose order is theirs, infinities and NaN last
+  const Tile t = tile_of(rows, pool, Hkv, unit);
+  const int lane = threadIdx.x & 63, col = lane % TPR * 8;
+  uint32_t* const k_image = image[wave];
+  uint32_t* const v_image = k_image + kWords;
+  float k[kRounds][8], v[kRounds][8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) most = max(most, __float_as_uint(x[i]) & 0x7fffffffu);
-  if (p.is_v) {
-    most = row_max<D>(most);
-    const bool number = most < kInfBits;
-    const float s = value_scale(number ? __uint_as_float(most) : 0.f), inv = 1.f / s;
+  for (int i = 0; i < kRounds; ++i) {
+    const int key = min(max(i * kKeys + lane / TPR, t.from), t.to - 1);  // one of the request's is read in its place
+    load_row8(k_new + (t.row0 + key) * k_stride + t.head * D + col, k[i]);
+    load_row8(v_new + (t.row0 + key) * v_stride + t.head * D + col, v[i]);
+  }
+  uint8_t* const k_scale = pool.k_scale + t.block * (2 * D) + t.key0 / kTile;
+  uint16_t* const v_scale = pool.v_scale + t.block * kKeyBlock4 + t.key0;
+  // A tile of few keys skips the rounds without any; a whole one has no branches.
+  auto encode = [&](auto whole) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = number ? over_scale<T>(x[i], s, inv) : 0.f;
-    if (p.mine) {
-      reinterpret_cast<uint32_t*>(pool.v)[p.block * (8 * D) + v_dword(p.key, p.col)] = encode8_fp4(x, 1.f);
-      if (p.col == 0) pool.v_scale[p.block * 64 + p.key] = number ? (uint16_t)(__float_as_uint(s) >> 16) : 0x7fc0;
+    for (int i = 0; i < kRounds; ++i) {
+      if (!decltype(whole)::value && (i * kKeys >= t.to || (i + 1) * kKeys <= t.from)) continue;
+      const int key = i * kKeys + lane / TPR;
+      const bool mine = key >= t.from && key < t.to;
+      uint32_t most_k = 0, most_v = 0;  // of the magnitudes' bits, whose order is theirs, infinities and NaN last
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        most_k = max(most_k, __float_as_uint(k[i][e]) & 0x7fffffffu);
+        most_v = max(most_v, __float_as_uint(v[i][e]) & 0x7fffffffu);
+      }
+      most_k = quad_max(most_k);
+      most_v = row_max<D>(most_v);
+      const bool k_number = most_k < kInfBits, v_number = most_v < kInfBits;
+      const int byte = key_scale(k_number ? most_k : 0u);
+      const float s = value_scale(v_number ? __uint_as_float(most_v) : 0.f), inv = 1.f / s;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[i][e] = over_scale<T>(v[i][e], s, inv);
+      k_image[k_dword<D>(key, col)] = k_number ? encode8_fp4(k[i], __uint_as_float((uint32_t)byte << 23)) : 0u;
+      v_image[v_dword(key, col)] = v_number ? encode8_fp4(v[i], 1.f) : 0u;
+      if (mine && col % kGroup4 == 0) k_scale[(col / kGroup4 * 16 + key) * 4] = k_number ? (uint8_t)byte : 255;  // [D/32][16 r][4 t]
+      if (mine && col == 0) v_scale[key] = v_number ? (uint16_t)(__float_as_uint(s) >> 16) : 0x7fc0;
     }
-  } else {
-    most = quad_max(most);
-    const bool number = most < kInfBits;
-    const int e = key_scale(number ? most : 0u);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = number ? x[i] : 0.f;
-    if (p.mine) {
-      reinterpret_cast<uint32_t*>(pool.k)[p.block * (8 * D) + k_dword<D>(p.key, p.col)] =
-          encode8_fp4(x, __uint_as_float((uint32_t)e << 23));
-      if (p.col % kGroup4 == 0) pool.k_scale[p.block * (2 * D) + k_scale_byte(p.key, p.col)] = number ? (uint8_t)e : 255;
+  };
+  if (t.to - t.from == kTile) encode(std::true_type());
+  else encode(std::false_type());
+  lds_wait();  // the wave's own image is whole
+  uint8_t* const k_out = pool.k + t.block * (32 * D) + t.key0 * (D / 2);
+  uint8_t* const v_out = pool.v + t.block * (32 * D) + t.key0 * 8;
+  {
+    // D / 8 bytes of each key and column group of K.
+    const int key = lane % kTile;
+    if (key >= t.from && key < t.to) {
+      if (D == 128)
+        reinterpret_cast<u32x4*>(k_out)[lane] = reinterpret_cast<const u32x4*>(k_image)[lane];
+      else
+        reinterpret_cast<u32x2*>(k_out)[lane] = reinterpret_cast<const u32x2*>(k_image)[lane];
     }
+  }
+  if (lane < D / 2) {  // two keys of 16 columns of V: 16 bytes
+    const int i = lane / 8, key = lane % 8 * 2;
+    const u32x4 w = reinterpret_cast<const u32x4*>(v_image)[lane];
+    uint8_t* const dst = v_out + i * 512 + key * 8;
+    const bool a = key >= t.from && key < t.to, b = key + 1 >= t.from && key + 1 < t.to;
+    if (a && b)
+      *reinterpret_cast<u32x4*>(dst) = w;
+    else if (a)
+      *reinterpret_cast<u32x2*>(dst) = u32x2{w[0], w[1]};
+    else if (b)
+      *reinterpret_cast<u32x2*>(dst + 8) = u32x2{w[2], w[3]};
   }
 }
 
@@ -150,35 +184,66 @@ __device__ __forceinline__ void decode2(uint32_t codes, float scale, float (&x)[
   x[2 * sel] = v[0];
   x[2 * sel + 1] = v[1];
 }
+__device__ __forceinline__ void decode8(uint32_t codes, float scale, float (&x)[8]) {
+  decode2<0>(codes, scale, x);
+  decode2<1>(codes, scale, x);
+  decode2<2>(codes, scale, x);
+  decode2<3>(codes, scale, x);
+}
 
 template <typename T, int D>
 __global__ __launch_bounds__(kRowThreads)
-void kv4_read_kernel(Kv4Rows rows, Kv4Pool pool, int Hkv, int nunits, int unit0, T* __restrict__ k_out, int64_t k_stride,
+void kv4_read_kernel(Kv4Rows rows, Kv4Pool pool, int Hkv, int nunits, T* __restrict__ k_out, int64_t k_stride,
                      T* __restrict__ v_out, int64_t v_stride) {
-  const int unit = unit0 + blockIdx.x * (kRowThreads / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  constexpr int TPR = D / 8, kKeys = kWave / TPR;
+  constexpr int kRounds = kTile / kKeys;
+  constexpr int kWords = kTile * D / 8;
+  __shared__ __align__(16) uint32_t image[kRowThreads / kWave][2 * kWords];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int unit = blockIdx.x * (kRowThreads / kWave) + wave;
   if (unit >= nunits) return;
-  const Place<D> p = place_of<D>(rows, pool, Hkv, unit);
-  const uint32_t codes = reinterpret_cast<const uint32_t*>(
-      p.is_v ? pool.v : pool.k)[p.block * (8 * D) + (p.is_v ? v_dword(p.key, p.col) : k_dword<D>(p.key, p.col))];
-  const float scale =
-      p.is_v ? bf16_to_f32(pool.v_scale[p.block * 64 + p.key])
-             : __uint_as_float((uint32_t)pool.k_scale[p.block * (2 * D) + k_scale_byte(p.key, p.col)] << 23);
-  float x[8];
-  const float pow2 = p.is_v ? 1.f : scale;
-  decode2<0>(codes, pow2, x);
-  decode2<1>(codes, pow2, x);
-  decode2<2>(codes, pow2, x);
-  decode2<3>(codes, pow2, x);
+  const Tile t = tile_of(rows, pool, Hkv, unit);
+  const int lane = threadIdx.x & 63, col = lane % TPR * 8;
+  uint32_t* const k_image = image[wave];
+  uint32_t* const v_image = k_image + kWords;
+  const uint8_t* const k_in = pool.k + t.block * (32 * D) + t.key0 * (D / 2);
+  const uint8_t* const v_in = pool.v + t.block * (32 * D) + t.key0 * 8;
+  const uint8_t* const k_scale = pool.k_scale + t.block * (2 * D) + t.key0 / kTile;
+  const uint16_t* const v_scale = pool.v_scale + t.block * kKeyBlock4 + t.key0;
+  float ks[kRounds], vs[kRounds];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = p.is_v ? x[i] * scale : x[i];
-  if (p.mine) store_row8((p.is_v ? v_out + p.row * v_stride : k_out + p.row * k_stride) + p.head * D + p.col, x);
+  for (int i = 0; i < kRounds; ++i) {
+    const int key = i * kKeys + lane / TPR;
+    ks[i] = __uint_as_float((uint32_t)k_scale[(col / kGroup4 * 16 + key) * 4] << 23);
+    vs[i] = bf16_to_f32(v_scale[key]);
+  }
+  if (D == 128)
+    reinterpret_cast<u32x4*>(k_image)[lane] = reinterpret_cast<const u32x4*>(k_in)[lane];
+  else
+    reinterpret_cast<u32x2*>(k_image)[lane] = reinterpret_cast<const u32x2*>(k_in)[lane];
+  if (lane < D / 2) reinterpret_cast<u32x4*>(v_image)[lane] = *reinterpret_cast<const u32x4*>(v_in + lane / 8 * 512 + lane % 8 * 16);
+  lds_wait();
+#pragma unroll
+  for (int i = 0; i < kRounds; ++i) {
+    const int key = i * kKeys + lane / TPR;
+    const bool mine = key >= t.from && key < t.to;
+    const int64_t row = t.row0 + key;
+    if (i * kKeys >= t.to || (i + 1) * kKeys <= t.from) continue;
+    float x[8];
+    decode8(k_image[k_dword<D>(key, col)], ks[i], x);
+    if (mine && k_out != nullptr) store_row8(k_out + row * k_stride + t.head * D + col, x);
+    decode8(v_image[v_dword(key, col)], 1.f, x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] *= vs[i];
+    if (mine && v_out != nullptr) store_row8(v_out + row * v_stride + t.head * D + col, x);
+  }
 }
 
 }  // namespace
 
 hipError_t launch_kv4_append(const Kv4Rows& r, const Kv4Pool& pool, int Hkv, int D, bool f32, const void* k_new,
                              int64_t k_stride, const void* v_new, int64_t v_stride, hipStream_t stream) {
-  const int nunits = r.prefix[r.nreq] * Hkv * 2;
+  const int nunits = r.prefix[r.nreq] * Hkv;
   const dim3 grid((nunits + kRowThreads / kWave - 1) / (kRowThreads / kWave)), block(kRowThreads);
 #define SDV_APPEND(T, DIM)                                                                                       \
   hipLaunchKernelGGL((kv4_append_kernel<T, DIM>), grid, block, 0, stream, r, pool, Hkv, nunits,                  \
@@ -198,11 +263,10 @@ hipError_t launch_kv4_append(const Kv4Rows& r, const Kv4Pool& pool, int Hkv, int
 
 hipError_t launch_kv4_read(const Kv4Rows& r, const Kv4Pool& pool, int Hkv, int D, bool f32, void* k_out,
                            int64_t k_stride, void* v_out, int64_t v_stride, hipStream_t stream) {
-  const int half = r.prefix[r.nreq] * Hkv;  // units of K; those of V follow
-  const int begin = k_out != nullptr ? 0 : half, end = v_out != nullptr ? 2 * half : half;
-  const dim3 grid((end - begin + kRowThreads / kWave - 1) / (kRowThreads / kWave)), block(kRowThreads);
+  const int nunits = r.prefix[r.nreq] * Hkv;
+  const dim3 grid((nunits + kRowThreads / kWave - 1) / (kRowThreads / kWave)), block(kRowThreads);
 #define SDV_READ(T, DIM)                                                                                         \
-  hipLaunchKernelGGL((kv4_read_kernel<T, DIM>), grid, block, 0, stream, r, pool, Hkv, end, begin,                \
+  hipLaunchKernelGGL((kv4_read_kernel<T, DIM>), grid, block, 0, stream, r, pool, Hkv, nunits,                    \
                      static_cast<T*>(k_out), k_stride, static_cast<T*>(v_out), v_stride)
   if (f32 && D == 128) {
     SDV_READ(float, 128);

@@ -7,6 +7,8 @@
 // by as many threads as it has, and kept in LDS; a thread holds eight columns of a head.
 // Angles are reduced in float64, in revolutions: a float32 product of a far position
 // would be off by whole radians.
+#include <algorithm>
+
 #include "fp4.h"
 
 namespace sdv {
@@ -14,6 +16,7 @@ namespace sdv {
 namespace {
 
 constexpr int kRopeThreads = 256;
+constexpr int kRopeGroups = 2048;
 
 // Sum over the threads of a head.
 template <int D>
@@ -54,7 +57,25 @@ __device__ __forceinline__ void normed(float (&x)[8], const float (&w)[8], float
   for (int i = 0; i < 8; ++i) x[i] = (float)((double)x[i] * r * (double)w[i]);
 }
 
-template <typename T, int D, bool INTERLEAVED>
+// Eight of a weight's columns, which every head reads again.
+__device__ __forceinline__ void load_weight(const uint16_t* p, float (&w)[8]) {
+  const u32x4 r = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    w[2 * i] = __uint_as_float(r[i] << 16);
+    w[2 * i + 1] = __uint_as_float(r[i] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void load_weight(const float* p, float (&w)[8]) {
+  const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    w[i] = a[i];
+    w[4 + i] = b[i];
+  }
+}
+
+template <typename T, int D, bool INTERLEAVED, bool NORM>
 __global__ __launch_bounds__(kRopeThreads)
 void qk_rope_kernel(RopeArgs a, const T* q, const T* k, const int32_t* __restrict__ positions,
                     const float* __restrict__ inv_freq, const T* __restrict__ q_weight,
@@ -90,20 +111,19 @@ void qk_rope_kernel(RopeArgs a, const T* q, const T* k, const int32_t* __restric
     const T* src = (mine && is_k ? k + row * a.k_stride : q + row * a.q_stride) + hc * D + col;
     float x[8];
     load_row8(src, x);
-    const T* weight = mine && is_k ? k_weight : q_weight;
     float y[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = x[i];
-    float w[8];
-    if (weight != nullptr) {
-      load_row8(weight + col, w);
-    } else {
+    if (NORM) {
+      const T* weight = mine && is_k ? k_weight : q_weight;
+      float w[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) w[i] = 1.f;
-    }
-    normed<D>(y, w, a.eps);
+      if (weight != nullptr) load_weight(weight + col, w);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = weight != nullptr ? y[i] : x[i];
+      for (int i = 0; i < 8; ++i) y[i] = x[i];
+      normed<D>(y, w, a.eps);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = weight != nullptr ? y[i] : x[i];
+    }
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[i] = INTERLEAVED ? x[i ^ 1] : __shfl(x[i], other & 63);
 #pragma unroll
@@ -117,16 +137,24 @@ void qk_rope_kernel(RopeArgs a, const T* q, const T* k, const int32_t* __restric
 hipError_t launch_qk_rope(const RopeArgs& a, int D, bool f32, bool interleaved, const void* q, const void* k,
                           const int32_t* positions, const float* inv_freq, const void* q_weight, const void* k_weight,
                           void* q_out, void* k_out, hipStream_t stream) {
-  const dim3 grid(a.rows), block(kRopeThreads);
-#define SDV_ROPE(T, DIM, INTER)                                                                                   \
-  hipLaunchKernelGGL((qk_rope_kernel<T, DIM, INTER>), grid, block, 0, stream, a, static_cast<const T*>(q),         \
+  // A row's heads are shared among workgroups until there are kRopeGroups.
+  const int64_t passes = (a.Hq + a.Hkv + kRopeThreads * 8 / D - 1) / (kRopeThreads * 8 / D);
+  const int64_t shares = std::max<int64_t>(1, std::min({passes, int64_t(kRopeGroups) / a.rows, int64_t(65535)}));
+  const dim3 grid(a.rows, static_cast<unsigned>(shares)), block(kRopeThreads);
+  const bool norm = q_weight != nullptr || k_weight != nullptr;
+#define SDV_ROPE(T, DIM, INTER, NORM)                                                                             \
+  hipLaunchKernelGGL((qk_rope_kernel<T, DIM, INTER, NORM>), grid, block, 0, stream, a, static_cast<const T*>(q),         \
                      static_cast<const T*>(k), positions, inv_freq, static_cast<const T*>(q_weight),               \
                      static_cast<const T*>(k_weight), static_cast<T*>(q_out), static_cast<T*>(k_out))
 #define SDV_ROPE_DIM(T, DIM)        \
-  if (interleaved) {                \
-    SDV_ROPE(T, DIM, true);         \
+  if (interleaved && norm) {        \
+    SDV_ROPE(T, DIM, true, true);   \
+  } else if (interleaved) {         \
+    SDV_ROPE(T, DIM, true, false);  \
+  } else if (norm) {                \
+    SDV_ROPE(T, DIM, false, true);  \
   } else {                          \
-    SDV_ROPE(T, DIM, false);        \
+    SDV_ROPE(T, DIM, false, false); \
   }
   if (f32 && D == 128) {
     SDV_ROPE_DIM(float, 128)
