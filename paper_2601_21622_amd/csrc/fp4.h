@@ -41,7 +41,8 @@ hipError_t launch_kv4_read(const Kv4Rows& r, const Kv4Pool& pool, int Hkv, int D
                            int64_t k_stride, void* v_out, int64_t v_stride, hipStream_t stream);
 
 // Attention over a 4-bit cache.  kv4_shape fills an AttnShape for these lengths
-// (chunks are whole 64-key blocks); kv4_max_chunks bounds the chunk count of any
+// (chunks are whole 64-key blocks; none, chunk_keys 0, where a workgroup takes a whole
+// request and writes the output itself); kv4_max_chunks bounds the chunk count of any
 // lengths up to max_kv_len.  AttnBatch is used without kv_off and pages.
 AttnShape kv4_shape(int G, int Hq, int Hkv, int D, float scale, const int32_t* kv_len, int B);
 int64_t kv4_max_chunks(int Hkv, int D, int B, int64_t max_kv_len);

@@ -188,7 +188,7 @@ int sd_verify_attention_kv4(const sd_dims_t* d, const void* q, const sd_kv4_cach
   for (int b = 0; b < d->batch; ++b)
     if (kv_len[b] < G || !length_ok(cache, kv_len[b])) return SD_ERR_INVALID_ARGUMENT;
   const AttnShape s = kv4_shape(G, d->n_q_heads, d->n_kv_heads, d->head_dim, scale, kv_len, d->batch);
-  const int64_t chunks = count_chunks(kv_len, d->batch, s.chunk_keys);
+  const int64_t chunks = s.chunk_keys > 0 ? count_chunks(kv_len, d->batch, s.chunk_keys) : 0;
   if (chunks * s.Hkv * s.row_groups > kMaxGrid) return SD_ERR_UNSUPPORTED;
   if (workspace_bytes < attention_ws(s, chunks)) return SD_ERR_WORKSPACE;
   const AttnPartials parts = attn_carve(workspace, chunks, s.Hkv, s.rows, s.D);
@@ -204,7 +204,7 @@ int sd_verify_attention_kv4(const sd_dims_t* d, const void* q, const sd_kv4_cach
     bt.parent = d->gamma > 0 ? parent : nullptr;
     for (int i = 0; i < bt.nreq; ++i) {
       bt.kv_len[i] = kv_len[r0 + i];
-      bt.chunk_prefix[i + 1] = bt.chunk_prefix[i] + (kv_len[r0 + i] + s.chunk_keys - 1) / s.chunk_keys;
+      bt.chunk_prefix[i + 1] = s.chunk_keys > 0 ? bt.chunk_prefix[i] + (kv_len[r0 + i] + s.chunk_keys - 1) / s.chunk_keys : 0;
     }
     if (launch_kv4_attention(s, bt, pool, bt.chunk_prefix[bt.nreq], q, parts, out, stm) != hipSuccess)
       return SD_ERR_HIP;

@@ -31,6 +31,7 @@ namespace sdv {
 namespace {
 
 constexpr int kMaxTiles4 = 64;  // blocks per chunk: one lane holds one block's page
+constexpr int kManyChunks = 16;  // chunks of a request that one thread joins
 constexpr float kNoKey4 = -3.402823466e38f;  // reference of a row that has seen no key: no score lies below it
 constexpr float kGrow = 256.f;      // sum of a lane's 16 weights of a block that sets a new reference
 constexpr float kCareful = 65536.f;  // log2 magnitude of a reference from which sums start at zero
@@ -278,27 +279,22 @@ __device__ __forceinline__ bool fold_block4(Wave4<RB, D>& w, const unsigned char
   return true;
 }
 
-// One work item: rows from `row0` on of a chunk and KV head; a ring of N blocks.
+// Folds blocks blk0 .. blk0 + ntiles - 1 (at most 64) of request `lo` of the launch and one KV head
+// into the rows from `row0` on; a ring of N blocks.
 template <int RB, int D, int N>
-__device__ __forceinline__ void attend_item(const AttnShape& s, const AttnBatch& bt, const Kv4Pool& pool,
-                                            const uint16_t* __restrict__ q, const AttnPartials& parts, unsigned char* ring,
-                                            int c, int head, int row0) {
+__device__ __forceinline__ void fold_keys(Wave4<RB, D>& w, const AttnShape& s, const AttnBatch& bt, const Kv4Pool& pool,
+                                          const uint16_t* __restrict__ q, unsigned char* ring, int lo, int head, int row0,
+                                          int blk0, int ntiles) {
   using R = Ring4<D>;
   const int lane = threadIdx.x & 63;
   const int lr = lane & 15, lg = lane >> 4;
-  // The largest request with chunk_prefix <= c: one load, a request per lane.
-  const int prefix = lane < bt.nreq ? bt.chunk_prefix[lane] : INT32_MAX;
-  const int lo = __popcll(__ballot(prefix <= c)) - 1;
   const int req = bt.req0 + lo;
-  const int end = bt.kv_len[lo], first = end - s.G;
-  const int key_begin = (c - __builtin_amdgcn_readlane(prefix, lo)) * s.chunk_keys;
-  const int key_end = min(key_begin + s.chunk_keys, end);
-  const int ntiles = __builtin_amdgcn_readfirstlane((key_end - key_begin + kKeyBlock4 - 1) / kKeyBlock4);
-  const int blk0 = key_begin / kKeyBlock4;
+  const int first = bt.kv_len[lo] - s.G;
+  const int key_begin = blk0 * kKeyBlock4;
 
-  // Lane j: where block j of the chunk lies.
+  // Lane j: where block j lies.
   const int shift = pool.page_shift - 6;
-  const int blk = blk0 + min(lane, ntiles - 1);
+  const int blk = blk0 + min(lane, max(ntiles - 1, 0));
   int page = pool.table[(int64_t)req * pool.max_pages + (blk >> shift)];
   page = min(max(page, 0), pool.num_pages - 1);
   const int64_t at = (((int64_t)page * s.Hkv + head) << shift) + (blk & ((1 << shift) - 1));
@@ -323,7 +319,6 @@ __device__ __forceinline__ void attend_item(const AttnShape& s, const AttnBatch&
       fetch(t, true);
     }
 
-  Wave4<RB, D> w;
   const int whole = __builtin_amdgcn_readfirstlane(min(max((first + 1 - key_begin) / kKeyBlock4, 0), ntiles));  // blocks that every row sees whole
   uint64_t masks = 1;  // a chunk of whole blocks ends with position 0 at the latest: all rows see it
   if (whole < ntiles) masks = position_mask(bt.parent != nullptr ? bt.parent + (int64_t)req * (s.G - 1) : nullptr, s.G);
@@ -372,17 +367,32 @@ __device__ __forceinline__ void attend_item(const AttnShape& s, const AttnBatch&
     return done;
   };
   int t = 0;
-  arrived(0);
-  for (;;) {
+  if (ntiles > 0) arrived(0);
+  while (t < ntiles) {
     careful = set_reference<RB, D>(w, place(t), s.scale_log2, offset(t));
     own = t;
     bool done = true;
     if (!careful)
       for (; t < whole && done; t += done) done = step(__builtin_amdgcn_readfirstlane(t), Kind<false>());
     for (; t < ntiles && done; t += done) done = step(__builtin_amdgcn_readfirstlane(t), Kind<true>());
-    if (done) break;
   }
+}
 
+// One work item: rows from `row0` on of a chunk and KV head.
+template <int RB, int D, int N>
+__device__ __forceinline__ void attend_item(const AttnShape& s, const AttnBatch& bt, const Kv4Pool& pool,
+                                            const uint16_t* __restrict__ q, const AttnPartials& parts, unsigned char* ring,
+                                            int c, int head, int row0) {
+  const int lane = threadIdx.x & 63;
+  const int lr = lane & 15, lg = lane >> 4;
+  // The largest request with chunk_prefix <= c: one load, a request per lane.
+  const int prefix = lane < bt.nreq ? bt.chunk_prefix[lane] : INT32_MAX;
+  const int lo = __popcll(__ballot(prefix <= c)) - 1;
+  const int key_begin = (c - __builtin_amdgcn_readlane(prefix, lo)) * s.chunk_keys;
+  const int key_end = min(key_begin + s.chunk_keys, bt.kv_len[lo]);
+  Wave4<RB, D> w;
+  fold_keys<RB, D, N>(w, s, bt, pool, q, ring, lo, head, row0, key_begin / kKeyBlock4,
+                      __builtin_amdgcn_readfirstlane((key_end - key_begin + kKeyBlock4 - 1) / kKeyBlock4));
   const int64_t slot = (int64_t)(bt.chunk_base + c) * s.Hkv + head;
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
@@ -420,12 +430,150 @@ void kv4_attn_kernel(AttnShape s, AttnBatch bt, Kv4Pool pool, int nchunks, int f
     attend_item<(UNEVEN ? RB - 1 : RB), D, N>(s, bt, pool, q, parts, ring, c, head, (rg * (RB - 1) + full) * 16);
 }
 
-int max_blocks4(int) { return 5; }  // 16-row blocks of a wave
+// Four columns of a row's output, num / den.
+__device__ __forceinline__ void store_four(uint16_t* out, const AttnShape& s, int req, int head, int row, int d, f32x4 num,
+                                           float den) {
+  const int j = row / s.group, h = head * s.group + row - j * s.group;
+  const float inv = 1.f / den;
+  const bf16x2 x = __builtin_convertvector((f32x2{num[0] * inv, num[1] * inv}), bf16x2);
+  const bf16x2 y = __builtin_convertvector((f32x2{num[2] * inv, num[3] * inv}), bf16x2);
+  *reinterpret_cast<u32x2*>(out + (((int64_t)req * s.G + j) * s.Hq + h) * s.D + d) =
+      u32x2{__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, y)};
+}
 
+// A request's blocks shared among the W waves of a workgroup, which join their O in
+// LDS: no partials and no second launch, where a request's keys are few.
+template <int W, int D>
+__global__ __launch_bounds__(W * kWave, 2)
+void kv4_attn_join_kernel(AttnShape s, AttnBatch bt, Kv4Pool pool, const uint16_t* __restrict__ q,
+                          uint16_t* __restrict__ out) {
+  constexpr int kRing = 4 * Ring4<D>::kHalf, kRow = D + 4;  // bytes of a wave's ring; floats of a row of O, which spread over the banks
+  static_assert(16 * kRow * 4 <= kRing, "a wave's O takes its ring's place");
+  __shared__ __align__(1024) unsigned char ring[W * kRing];
+  __shared__ float ms[W][16], ls[W][16];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
+  const int per = 8 * s.row_groups;
+  const int item = blockIdx.x / per * 8 + (blockIdx.x & 7);
+  const int rg = blockIdx.x % per >> 3;
+  if (item >= bt.nreq * s.Hkv) return;
+  const int head = item % s.Hkv, lo = item / s.Hkv;
+  const int blocks = (bt.kv_len[lo] + kKeyBlock4 - 1) / kKeyBlock4;
+  const int from = blocks * wave / W, to = blocks * (wave + 1) / W;
+  unsigned char* const mine = ring + wave * kRing;
+  Wave4<1, D> w;
+  fold_keys<1, D, 2>(w, s, bt, pool, q, mine, lo, head, rg * 16, from, __builtin_amdgcn_readfirstlane(to - from));
+  lds_wait();
+  float* const o = reinterpret_cast<float*>(mine) + lr * kRow + 4 * lg;
+#pragma unroll
+  for (int db = 0; db < D / 16; ++db) *reinterpret_cast<f32x4*>(o + db * 16) = w.o[0][db];
+  const float l = sum_over_groups(w.l[0]);
+  if (lg == 0) {
+    ms[wave][lr] = w.m[0];
+    ls[wave][lr] = l;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < 16 * (D / 4); i += W * kWave) {
+    const int r = i / (D / 4), d = i % (D / 4) * 4, row = rg * 16 + r;
+    if (row >= s.rows) break;
+    float m = ms[0][r];
+#pragma unroll
+    for (int k = 1; k < W; ++k) m = fmaxf(m, ms[k][r]);
+    float den = 0.f;
+    f32x4 num = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < W; ++k) {
+      const float a = __builtin_amdgcn_exp2f((ms[k][r] - m) * s.scale_log2);
+      den = fmaf(a, ls[k][r], den);
+      num += a * *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(ring + k * kRing) + r * kRow + d);
+    }
+    store_four(out, s, bt.req0 + lo, head, row, d, num, den);
+  }
+}
+
+// 16-row blocks of a wave, at most; more rows are split over row groups, a wave each.
+int max_blocks4(int64_t blocks) { return blocks <= 24 * cu_count() ? 1 : blocks <= 40 * cu_count() ? 2 : 5; }
 int blocks_of4(int rows, int groups) { return ((rows + 15) / 16 + groups - 1) / groups; }
 
 // Workgroups (one wave, one item each) that run at once: what LDS and registers hold.
-int64_t places4(int) { return cu_count() * 8; }
+int64_t places4(int D, int most) {
+  const int per = most > 3 ? 4 : D == 128 ? 8 : most == 1 ? 16 : most == 2 ? 12 : 8;
+  return cu_count() * per;
+}
+
+// Whether requests are shared among the waves of one workgroup each (for 16 rows of a KV head):
+// `groups` of those workgroups, whose longest request has `longest` blocks and all `total`.
+// By what both ways take: the longest request's blocks, eight at once, against a second launch and
+// the chunks' even spread.  One head dimension's figures (us, joined / in chunks, requests of
+// one length, 8 KV heads): D = 128: 1 x 1,000 keys 9.2 / 10.2, 1 x 4,000 18.5 / 14.0, 4 x 4,000 of 72 rows
+// 19.5 / 23.4, 8 x 4,000 of one token 18.4 / 16.3, 32 x 1,000 10.4 / 14.8; D = 64: 13 x 1,500 of 48 rows 13.1 / 17.4,
+// 24 x 1,400 of 40 rows 16.9 / 20.4.  Not of more workgroups than run at once: 64 x 1,000 keys of one token,
+// D = 128, 20.8 / 18.8.
+bool joins(int64_t groups, int64_t longest, int64_t total, int D) {
+  if (longest > 8 * kMaxTiles4) return false;
+  return D == 128 ? groups <= cu_count() && 160 * longest < 3200 + total
+                  : groups <= cu_count() * 5 / 2 && 240 * longest < 5000 + total;
+}
+
+// Joins many partials: the chunks of each (request, position, head) are dealt to the slices of a workgroup,
+// whose sums join in slice order.  A thread holds four columns.  One request of 30,000 keys in 60 chunks,
+// one token, D = 128: 21 us the whole call.
+template <int D>
+__global__ __launch_bounds__(256)
+void kv4_merge_many_kernel(AttnShape s, AttnBatch bt, AttnPartials parts, uint16_t* __restrict__ out) {
+  constexpr int TPR = D / 4, S = 256 / TPR;
+  __shared__ float ms[S], ls[S];
+  __shared__ __align__(16) f32x4 os[S][TPR];
+  const int row = blockIdx.x, head = blockIdx.y, b = blockIdx.z;
+  const int slice = threadIdx.x / TPR, d = threadIdx.x % TPR;
+  const int c0 = bt.chunk_base + bt.chunk_prefix[b], c1 = bt.chunk_base + bt.chunk_prefix[b + 1];
+  float m = kNoKey4, den = 0.f;
+  f32x4 num = {0.f, 0.f, 0.f, 0.f};
+  for (int c = c0 + slice; c < c1; c += 4 * S) {
+    float mc[4], lc[4];
+    f32x4 oc[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int64_t at = ((int64_t)min(c + k * S, c1 - 1) * s.Hkv + head) * s.rows + row;
+      mc[k] = parts.m[at];
+      lc[k] = parts.l[at];
+      oc[k] = *reinterpret_cast<const f32x4*>(parts.o + at * D + 4 * d);
+    }
+    float mn = m;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) mn = fmaxf(mn, mc[k]);
+    const float alpha = __builtin_amdgcn_exp2f((m - mn) * s.scale_log2);
+    den *= alpha;
+    num *= alpha;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (c + k * S < c1) {
+        const float a = __builtin_amdgcn_exp2f((mc[k] - mn) * s.scale_log2);
+        den = fmaf(a, lc[k], den);
+        num += a * oc[k];
+      }
+    m = mn;
+  }
+  if (d == 0) {
+    ms[slice] = m;
+    ls[slice] = den;
+  }
+  os[slice][d] = num;
+  __syncthreads();
+  if (slice != 0) return;
+  float mn = ms[0];
+#pragma unroll
+  for (int k = 1; k < S; ++k) mn = fmaxf(mn, ms[k]);
+  den = 0.f;
+  num = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int k = 0; k < S; ++k) {
+    const float a = __builtin_amdgcn_exp2f((ms[k] - mn) * s.scale_log2);
+    den = fmaf(a, ls[k], den);
+    num += a * os[k][d];
+  }
+  store_four(out, s, bt.req0 + b, head, row, 4 * d, num, den);
+}
 
 }  // namespace
 
@@ -437,20 +585,38 @@ AttnShape kv4_shape(int G, int Hq, int Hkv, int D, float scale, const int32_t* k
   s.D = D;
   s.group = Hq / Hkv;
   s.rows = G * s.group;
-  const int b = (s.rows + 15) / 16;
-  s.row_groups = (b + max_blocks4(D) - 1) / max_blocks4(D);
+  int64_t blocks = 0;
+  for (int i = 0; i < B; ++i) blocks += (kv_len[i] + kKeyBlock4 - 1) / kKeyBlock4;
+  const int b = (s.rows + 15) / 16, upto = max_blocks4(blocks * Hkv);
+  s.row_groups = (b + upto - 1) / upto;
   s.scale_log2 = scale * kLog2e;
+  int longest = 0;
+  for (int i = 0; i < B; ++i) longest = std::max(longest, kv_len[i]);
+  longest = (longest + kKeyBlock4 - 1) / kKeyBlock4;
+  if (joins(int64_t(B) * Hkv * b, longest, blocks * Hkv * b, D)) {
+    s.row_groups = b;
+    s.chunk_keys = 0;
+    return s;
+  }
   // For a half to four rounds of items over the CUs' places the shortest chunk that
-  // fits them; of these the one that is done first, counted in keys.
-  const int64_t slots = places4(D);
-  const int64_t start = 192 + 2 * s.rows;
+  // fits them; of these the one that is done first, in ns.  A wave takes kAlone a block by itself and no less than
+  // kShared for each of those on its SIMD (where the caches' stream or the SIMD's own instructions bound it).  Items in
+  // more rounds are handed out as places come free, and the last ones end half a chunk apart.  Each item
+  // costs its start, and its partial is written and read at 5 TB/s.
+  // More items than four rounds only with the longest chunk: the workspace holds no more partials.
+  const int most_rb = blocks_of4(s.rows, s.row_groups);
+  const int64_t slots = places4(D, most_rb), simds = cu_count() * 4;
+  static const int kAlone[2][5] = {{1380, 1700, 2200, 2750, 3400}, {750, 950, 1300, 1700, 2250}};
+  static const int kShared[2][5] = {{1270, 1500, 1850, 2750, 3400}, {650, 800, 1100, 1700, 2250}};
+  const int64_t alone = kAlone[D == 64][most_rb - 1], shared = kShared[D == 64][most_rb - 1];
+  const int64_t start = 1500;
   auto items = [&](int tiles) {
     const int keys = tiles * kKeyBlock4;
     int64_t n = 0;
     for (int i = 0; i < B; ++i) n += (kv_len[i] + keys - 1) / keys;
     return n * Hkv * s.row_groups;
   };
-  const int64_t total = items(1) * kKeyBlock4;
+  const int64_t total = blocks * Hkv * s.row_groups;
   int64_t best = INT64_MAX;
   int most = kMaxTiles4;
   s.chunk_keys = kMaxTiles4 * kKeyBlock4;
@@ -462,9 +628,10 @@ AttnShape kv4_shape(int G, int Hq, int Hkv, int D, float scale, const int32_t* k
       const int mid = (lo + hi) / 2;
       if (items(mid) <= fit) hi = mid; else lo = mid + 1;
     }
-    const int64_t keys = int64_t(lo) * kKeyBlock4;
     const int64_t n = items(lo);
-    const int64_t cost = (r <= 2 ? keys + start : (total + n * start) / slots + keys / 2) + n * s.rows * 16 / slots;
+    const int64_t fold = n <= slots ? std::max(lo * alone, lo * shared * n / simds)
+                                    : total * shared / simds + lo * std::max(alone, shared * slots / simds) / 2;
+    const int64_t cost = fold + (n + slots - 1) / slots * start + n * (s.rows / s.row_groups) * (D + 2) * 8 / 5000;
     if (cost < best) {
       best = cost;
       s.chunk_keys = lo * kKeyBlock4;
@@ -476,13 +643,22 @@ AttnShape kv4_shape(int G, int Hq, int Hkv, int D, float scale, const int32_t* k
 }
 
 int64_t kv4_max_chunks(int Hkv, int D, int B, int64_t max_kv_len) {
-  const int64_t most = std::min(4 * places4(D) / Hkv, B * ((max_kv_len + kKeyBlock4 - 1) / kKeyBlock4));
+  const int64_t most = std::min(4 * places4(D, 1) / Hkv, B * ((max_kv_len + kKeyBlock4 - 1) / kKeyBlock4));
   const int64_t at_longest = B * ((max_kv_len + kMaxTiles4 * kKeyBlock4 - 1) / (kMaxTiles4 * kKeyBlock4));
   return std::max(most, at_longest);
 }
 
 hipError_t launch_kv4_attention(const AttnShape& s, const AttnBatch& batch, const Kv4Pool& pool, int nchunks,
                                 const void* q, AttnPartials parts, void* out, hipStream_t stream) {
+  if (s.chunk_keys == 0) {
+    const dim3 grid((batch.nreq * s.Hkv + 7) / 8 * 8 * s.row_groups);
+#define SDV_JOIN(W, DIM)                                                                                          \
+  hipLaunchKernelGGL((kv4_attn_join_kernel<W, DIM>), grid, dim3(W * kWave), 0, stream, s, batch, pool,            \
+                     static_cast<const uint16_t*>(q), static_cast<uint16_t*>(out))
+    if (s.D == 128) SDV_JOIN(8, 128); else SDV_JOIN(8, 64);
+#undef SDV_JOIN
+    return hipGetLastError();
+  }
   const dim3 grid((nchunks * s.Hkv + 7) / 8 * 8 * s.row_groups), block(kWave);
   const int blocks = (s.rows + 15) / 16, most = blocks_of4(s.rows, s.row_groups);
   const int full = blocks - (most - 1) * s.row_groups;  // row groups of `most` blocks
@@ -498,14 +674,22 @@ hipError_t launch_kv4_attention(const AttnShape& s, const AttnBatch& batch, cons
   if (most == 1) SDV_KV4(1, false);
   else if (most == 2 && full == s.row_groups) SDV_KV4(2, false);
   else if (most == 2) SDV_KV4(2, true);
-  else if (most == 3 && full == s.row_groups) SDV_KV4(3, false);
-  else if (most == 3) SDV_KV4(3, true);
-  else if (most == 4) SDV_KV4(4, false);
+  else if (most == 3) SDV_KV4(3, false);
+  else if (most == 4 && full == s.row_groups) SDV_KV4(4, false);
+  else if (most == 4) SDV_KV4(4, true);
   else SDV_KV4(5, false);
 #undef SDV_KV4
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  return launch_kv_merge(s, batch, parts, out, stream);
+  int chunks = 0;  // of a request
+  for (int b = 0; b < batch.nreq; ++b) chunks = std::max(chunks, batch.chunk_prefix[b + 1] - batch.chunk_prefix[b]);
+  if (chunks <= kManyChunks) return launch_kv_merge(s, batch, parts, out, stream);
+  const dim3 mgrid(s.rows, s.Hkv, batch.nreq);
+  if (s.D == 128)
+    hipLaunchKernelGGL(kv4_merge_many_kernel<128>, mgrid, dim3(256), 0, stream, s, batch, parts, static_cast<uint16_t*>(out));
+  else
+    hipLaunchKernelGGL(kv4_merge_many_kernel<64>, mgrid, dim3(256), 0, stream, s, batch, parts, static_cast<uint16_t*>(out));
+  return hipGetLastError();
 }
 
 }  // namespace sdv
