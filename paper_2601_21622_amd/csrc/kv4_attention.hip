@@ -501,18 +501,23 @@ int64_t places4(int D, int most) {
   return cu_count() * per;
 }
 
-// Whether requests are shared among the waves of one workgroup each (for 16 rows of a KV head):
-// `groups` of those workgroups, whose longest request has `longest` blocks and all `total`.
-// By what both ways take: the longest request's blocks, eight at once, against a second launch and
-// the chunks' even spread.  One head dimension's figures (us, joined / in chunks, requests of
-// one length, 8 KV heads): D = 128: 1 x 1,000 keys 9.2 / 10.2, 1 x 4,000 18.5 / 14.0, 4 x 4,000 of 72 rows
-// 19.5 / 23.4, 8 x 4,000 of one token 18.4 / 16.3, 32 x 1,000 10.4 / 14.8; D = 64: 13 x 1,500 of 48 rows 13.1 / 17.4,
-// 24 x 1,400 of 40 rows 16.9 / 20.4.  Not of more workgroups than run at once: 64 x 1,000 keys of one token,
-// D = 128, 20.8 / 18.8.
-bool joins(int64_t groups, int64_t longest, int64_t total, int D) {
-  if (longest > 8 * kMaxTiles4) return false;
-  return D == 128 ? groups <= cu_count() && 160 * longest < 3200 + total
-                  : groups <= cu_count() * 5 / 2 && 240 * longest < 5000 + total;
+// What a wave of one to five row blocks takes for a block of keys by itself, and what each of the waves on a SIMD takes at
+// least, in ns, at head dimension 128 and 64: 50 blocks a wave, one wave and two per SIMD.
+constexpr int kAlone[2][5] = {{1340, 1630, 2100, 2600, 3100}, {700, 1280, 1370, 1800, 2100}};
+constexpr int kShared[2][5] = {{1300, 1530, 1920, 2750, 3200}, {700, 1020, 1270, 1780, 2150}};
+
+// Whether requests are shared among the waves of one workgroup each (for 16 rows of a KV head)
+// instead of cut into chunks, which take `chunked` ns: by `groups` of those workgroups, the blocks of the longest
+// request, eight at once, and of all.  One launch less, against rows that are read once for each 16 and the longest
+// request's time.  In us, joined / in chunks, requests of one length, 8 KV heads; D = 128: 1 x 1,000 keys
+// 9.2 / 10.2, 1 x 4,000 18.5 / 10.4, 4 x 4,000 of 72 rows 19.5 / 23.4, 8 x 4,000 of one token 18.4 / 16.3,
+// 32 x 1,000 10.4 / 14.8; D = 64: 13 x 1,500 of 48 rows 13.1 / 17.4, 24 x 1,400 of 40 rows 16.9 / 20.4, 16 x 24,576 of
+// 72 rows 148 / 115.  Not of many more workgroups than run at once: 64 x 1,000 keys of one token, D = 128, 20.8 / 18.8.
+bool joins(int64_t groups, int64_t longest, int64_t total, int D, int64_t chunked) {
+  if (longest > 8 * kMaxTiles4 || groups > (D == 128 ? cu_count() : cu_count() * 5 / 2)) return false;
+  const int64_t mine = D == 128 ? std::max(longest * 200, total * kShared[0][0] / (4 * cu_count()))
+                                : std::max(longest * 190, total * kShared[1][0] / (4 * cu_count()));
+  return mine < chunked + 1000;
 }
 
 // Joins many partials: the chunks of each (request, position, head) are dealt to the slices of a workgroup,
@@ -593,11 +598,6 @@ AttnShape kv4_shape(int G, int Hq, int Hkv, int D, float scale, const int32_t* k
   int longest = 0;
   for (int i = 0; i < B; ++i) longest = std::max(longest, kv_len[i]);
   longest = (longest + kKeyBlock4 - 1) / kKeyBlock4;
-  if (joins(int64_t(B) * Hkv * b, longest, blocks * Hkv * b, D)) {
-    s.row_groups = b;
-    s.chunk_keys = 0;
-    return s;
-  }
   // For a half to four rounds of items over the CUs' places the shortest chunk that
   // fits them; of these the one that is done first, in ns.  A wave takes kAlone a block by itself and no less than
   // kShared for each of those on its SIMD (where the caches' stream or the SIMD's own instructions bound it).  Items in
@@ -606,8 +606,6 @@ AttnShape kv4_shape(int G, int Hq, int Hkv, int D, float scale, const int32_t* k
   // More items than four rounds only with the longest chunk: the workspace holds no more partials.
   const int most_rb = blocks_of4(s.rows, s.row_groups);
   const int64_t slots = places4(D, most_rb), simds = cu_count() * 4;
-  static const int kAlone[2][5] = {{1380, 1700, 2200, 2750, 3400}, {750, 950, 1300, 1700, 2250}};
-  static const int kShared[2][5] = {{1270, 1500, 1850, 2750, 3400}, {650, 800, 1100, 1700, 2250}};
   const int64_t alone = kAlone[D == 64][most_rb - 1], shared = kShared[D == 64][most_rb - 1];
   const int64_t start = 1500;
   auto items = [&](int tiles) {
@@ -617,7 +615,7 @@ AttnShape kv4_shape(int G, int Hq, int Hkv, int D, float scale, const int32_t* k
     return n * Hkv * s.row_groups;
   };
   const int64_t total = blocks * Hkv * s.row_groups;
-  int64_t best = INT64_MAX;
+  int64_t best = INT64_MAX / 2;
   int most = kMaxTiles4;
   s.chunk_keys = kMaxTiles4 * kKeyBlock4;
   for (int r : {1, 2, 4, 6, 8}) {  // half rounds
@@ -638,6 +636,10 @@ AttnShape kv4_shape(int G, int Hq, int Hkv, int D, float scale, const int32_t* k
     }
     most = lo;
     if (lo == 1) break;
+  }
+  if (joins(int64_t(B) * Hkv * b, longest, blocks * Hkv * b, D, best)) {
+    s.row_groups = b;
+    s.chunk_keys = 0;
   }
   return s;
 }
