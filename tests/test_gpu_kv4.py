@@ -276,6 +276,81 @@ def test_attention_of_long_caches(G, Hq, Hkv, D, lens):
     check_attention(got, q.double().numpy(), c.segments(lens), lens, Hkv, None, 1 / np.sqrt(D), "long")
 
 
+MANY = [3600, 3593, 3585, 3584, 3521, 3500]  # of 32 heads, more than 40 blocks of keys per CU
+SOME = MANY[:4]                              # more than 24
+
+
+@pytest.mark.parametrize("lens", [MANY, SOME], ids=["many", "some"])
+@pytest.mark.parametrize("G,D", [(3, 64), (5, 64), (8, 64), (9, 64), (14, 64), (3, 128), (5, 128), (8, 128), (9, 128), (11, 128),
+                                 (14, 128), (16, 128)])
+def test_attention_of_many_blocks(G, D, lens):
+    """Caches so large that a wave holds more than one block of 16 rows of a head: of 24, 40, 64, 72, 88, 112 and
+    128 rows, all in one wave, in several of one size and of two."""
+    rng = np.random.default_rng(10 * G + D)
+    Hkv = 32
+    c = filled(rng, lens, Hkv, D, 256)
+    q = torch.from_numpy(rng.normal(size=(len(lens), G, 8 * Hkv, D))).bfloat16()
+    got = attend(G, 8 * Hkv, Hkv, D, c, lens, q.cuda(), None, 1 / np.sqrt(D))
+    for b in (1, 3):  # each request against the oracle by itself
+        seg = fp4.kv4_segments(*c.host, c.table[b:b + 1], lens[b:b + 1])
+        check_attention(got[b:b + 1], q[b:b + 1].double().numpy(), seg, lens[b:b + 1], Hkv, None, 1 / np.sqrt(D),
+                        f"many blocks, request {b}")
+
+
+def place_of(c, b, at):
+    """Page and block of request b's key."""
+    return int(c.table[b][at // c.page]), at % c.page // 64
+
+
+@pytest.mark.parametrize("G,D", [(3, 64), (5, 64), (9, 64), (3, 128), (5, 128), (8, 128), (9, 128)])
+def test_jumps_and_nan_among_many_blocks(G, D):
+    """Scores that jump by hundreds from key to key (one product makes a score: exact but for the factors, 4 * 2^-24 of
+    512 log2 e, 2e-4 of a weight), with several row blocks to a wave; one NaN value that positions 2 .. of one head see; one
+    head's queries 2^40 times as large, whose references are past 2^16."""
+    rng = np.random.default_rng(20 * G + D)
+    Hkv, lens, page = 32, MANY, 256
+    c = filled(rng, lens, Hkv, D, page)
+    column = fp4.k_index(D)[:, 0]
+    codes = np.zeros((*c.host[0].shape[:3], 64 * D), dtype=np.uint8)
+    codes[..., column] = rng.integers(1, 8, (*codes.shape[:3], 64))
+    c.host[0][...] = fp4.pack(codes)
+    del codes
+    c.host[2][...] = 127
+    c.host[2][..., :64] += rng.choice([0, 0, 4, 6], (*c.host[2].shape[:3], 64)).astype(np.uint8)
+    at, (head, far) = lens[0] - G + 2, (3, 5)
+    page_id, blk = place_of(c, 0, at)
+    clean = [a.copy() for a in c.host]
+    c.host[3][page_id, head, blk, at % 64] = 0x7fc0
+    c.upload()
+    q = torch.zeros((len(lens), G, 8 * Hkv, D), dtype=torch.bfloat16)
+    q[..., 0] = torch.from_numpy(rng.choice([1.0, -1.0, 0.5], q.shape[:3])).bfloat16()
+    q[:, :, 8 * far:8 * far + 8] *= 2.0 ** 40
+    got = attend(G, 8 * Hkv, Hkv, D, c, lens, q.cuda(), None, 1.0)
+    hit = got[0, 2:, 8 * head:8 * head + 8]
+    assert np.isnan(hit).all() and np.isnan(got).sum() == hit.size
+    for b in (0, 2):
+        seg = fp4.kv4_segments(*clean, c.table[b:b + 1], lens[b:b + 1])
+        if b == 0:  # the spoilt outputs: as the oracle's
+            ref = verify_attention(q[:1].double().numpy(), *seg, lens[:1], Hkv, 1.0)
+            got[0, 2:, 8 * head:8 * head + 8] = ref[0, 2:, 8 * head:8 * head + 8]
+        check_attention(got[b:b + 1], q[b:b + 1].double().numpy(), seg, lens[b:b + 1], Hkv, None, 1.0,
+                        f"jumps among many blocks, request {b}")
+
+
+@pytest.mark.parametrize("B,G,Hq,Hkv,D,most", [(12, 1, 16, 16, 128, 2500), (20, 4, 16, 8, 64, 1900), (70, 2, 4, 2, 128, 400), (70, 3, 32, 32, 64, 130)])
+def test_attention_of_requests_of_any_length(B, G, Hq, Hkv, D, most):
+    """Lengths from the step's own positions to many blocks in one batch, of requests that a workgroup takes each (the first
+    three) and that are cut into chunks; more requests than a launch holds."""
+    rng = np.random.default_rng(B + D)
+    lens = [G + int(x) for x in np.linspace(0, most - G, B)]
+    rng.shuffle(lens)
+    c = filled(rng, lens, Hkv, D, 64)
+    q = torch.from_numpy(rng.normal(size=(B, G, Hq, D))).bfloat16()
+    got = attend(G, Hq, Hkv, D, c, lens, q.cuda(), None, 1 / np.sqrt(D))
+    check_attention(got, q.double().numpy(), c.segments(lens), lens, Hkv, None, 1 / np.sqrt(D), "lengths")
+
+
+
 def key_rows(c, b, at):
     """The pool's place of request b's key."""
     blocks = c.page // 64
