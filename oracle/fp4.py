@@ -148,8 +148,8 @@ def kv4_segments(k, v, k_scale, v_scale, table, kv_len):
             for n0 in range(0, int(n), BLOCK):
                 p = int(table[b][n0 // BLOCK // blocks]), h, n0 // BLOCK % blocks
                 kk[n0:n0 + BLOCK] = VALUES[unpack(k[p])[ki]] * key_scales(k_scale[p], dim)
-                with np.errstate(invalid="ignore"):
-                vv[n0:n0 + BLOCK] = VALUES[unpack(v[p])[vi]] * bf16_value(v_scale[p])[:, None]
+                with np.errstate(invalid="ignore"):  # 0 times infinity, past the last key
+                    vv[n0:n0 + BLOCK] = VALUES[unpack(v[p])[vi]] * bf16_value(v_scale[p])[:, None]
             parts[0].append(kk[:int(n)].reshape(-1))
             parts[1].append(vv[:int(n)].reshape(-1))
         at += heads * int(n) * dim
