@@ -329,7 +329,12 @@ __device__ __forceinline__ void fold_keys(Wave4<RB, D>& w, const AttnShape& s, c
     // Lane group g: the columns whose codes it holds of a key.
     const uint16_t* src = q + (((int64_t)req * s.G + j) * s.Hq + h) * D + (D / 4) * lg;
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) w.q[rb][i] = load_bf16x8(src + 8 * i);
+    for (int i = 0; i < D / 32; ++i) {
+      w.q[rb][i] = load_bf16x8(src + 8 * i);
+      // With five row blocks in the accumulation half of the registers, where the products take it from: the compiler
+      // would move it to the other half for every block of keys.
+      if (RB == 5) asm volatile("" : "+a"(w.q[rb][i]));
+    }
     const uint32_t a = __shfl((uint32_t)masks, j), b = __shfl((uint32_t)(masks >> 32), j);
     w.sees[rb] = ((uint64_t)b << 32) | a;
     w.m[rb] = kNoKey4;
