@@ -195,6 +195,26 @@ __device__ __forceinline__ bool set_reference(Wave4<RB, D>& w, const unsigned ch
   return __ballot(large) != 0;
 }
 
+// O += P V: V's columns come out of LDS transposed.
+template <int RB, int D>
+__device__ __forceinline__ void add_products4(Wave4<RB, D>& w, const unsigned char* vp, const bf16x8 (&pf)[RB][2]) {
+  const int lane = lane_here(), lr = lane & 15, lg = lane >> 4;
+  const unsigned char* vl = vp + (16 * (lr / 4) + 4 * lg + lr % 4) * 8;
+  i32x2 v[D / 16];
+#pragma unroll
+  for (int db = 0; db < D / 16; ++db) v[db] = lds_read_tr4(vl + db * 512);
+  bf16x8 vf = widen8_fp4((uint32_t)v[0][0], 1.f);
+#pragma unroll
+  for (int n = 0; n < D / 8; ++n) {
+    const int db = n % (D / 16), hf = n / (D / 16);
+    const bf16x8 now = vf;
+    if (n + 1 < D / 8) vf = widen8_fp4((uint32_t)v[(n + 1) % (D / 16)][(n + 1) / (D / 16)], 1.f);  // under this fragment's products
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) w.o[rb][db] = mfma16x16x32(now, pf[rb][hf], w.o[rb][db]);
+    interleave4<RB, 4>();
+  }
+}
+
 // Folds one block into O and the sums; false, with nothing changed, when a row's scores outgrow its
 // reference (not asked where the reference is this block's own, `own`).  MASKED serves large references
 // too (`careful`: scores are summed from zero).  refill_k asks for the block that takes K's place.
@@ -262,27 +282,79 @@ __device__ __forceinline__ bool fold_block4(Wave4<RB, D>& w, const unsigned char
   for (int rb = 0; rb < RB; ++rb) w.l[rb] += sum[rb];
   lds_wait();  // K has been read
   refill_k();
-  const int lane = lane_here(), lr = lane & 15, lg = lane >> 4;
-  const unsigned char* vl = vp + (16 * (lr / 4) + 4 * lg + lr % 4) * 8;
-  i32x2 v[D / 16];
+  add_products4<RB, D>(w, vp, pf);
+  return true;
+}
+
+// The same for one row block, which sets the reference itself (`set`: this block's scores are in it from now on);
+// its registers allow the rescaling here.
+template <int D, bool MASKED, typename RefillK>
+__device__ __forceinline__ bool fold_block_one(Wave4<1, D>& w, const unsigned char* kp, const unsigned char* vp, float scale_log2,
+                                               int off, bool set, bool& careful, RefillK refill_k) {
+  const bool zero = set || (MASKED && careful);
+  const float base[1] = {w.m[0] > kNoKey4 && !zero ? -w.m[0] : 0.f};
+  const uint32_t ks = key_scales4<D>(kp);
+  f32x4 sc[2][1][2];
 #pragma unroll
-  for (int db = 0; db < D / 16; ++db) v[db] = lds_read_tr4(vl + db * 512);
-  bf16x8 vf = widen8_fp4((uint32_t)v[0][0], 1.f);
+  for (int hf = 0; hf < 2; ++hf) half_scores4<1, D, MASKED>(w, kp, hf, ks, off, base, sc[hf]);
+  const int lg = lane_here() >> 4;
+  u32x2 vs[4];
 #pragma unroll
-  for (int n = 0; n < D / 8; ++n) {
-    const int db = n % (D / 16), hf = n / (D / 16);
-    const bf16x8 now = vf;
-    if (n + 1 < D / 8) vf = widen8_fp4((uint32_t)v[(n + 1) % (D / 16)][(n + 1) / (D / 16)], 1.f);  // under this fragment's products
+  for (int t = 0; t < 4; ++t) vs[t] = *reinterpret_cast<const u32x2*>(vp + Ring4<D>::kCodes + (16 * t + 4 * lg) * 2);
+  if (set) {
+    float x = kNoKey4;
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) w.o[rb][db] = mfma16x16x32(now, pf[rb][hf], w.o[rb][db]);
-    interleave4<RB, 4>();
+    for (int t = 0; t < 4; ++t) {
+      const f32x4 v = sc[t / 2][0][t % 2];
+      x = fmaxf(fmaxf(x, fmaxf(v[0], v[1])), fmaxf(v[2], v[3]));
+    }
+    const float m = fmaxf(w.m[0], max_over_groups(x));
+    const float alpha = __builtin_amdgcn_exp2f((w.m[0] - m) * scale_log2);
+    w.m[0] = m;
+    w.l[0] *= alpha;
+#pragma unroll
+    for (int db = 0; db < D / 16; ++db) w.o[0][db] *= alpha;
+    careful = __ballot(m > kNoKey4 && fabsf(m) * scale_log2 >= kCareful) != 0;
   }
+  if (zero) {
+    const float m = w.m[0] > kNoKey4 ? w.m[0] : 0.f;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sc[t / 2][0][t % 2][r] -= m;
+  }
+  bf16x8 pf[1][2];
+  float sum = 0.f;
+  const uint64_t win = MASKED ? keys_seen(w.sees[0], off) : 0;
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const float scale = __uint_as_float(r & 1 ? vs[t][r / 2] & 0xffff0000u : vs[t][r / 2] << 16);
+      const float p = __builtin_amdgcn_exp2f(sc[t / 2][0][t % 2][r] * scale_log2);
+      sum += p;
+      float y = p * scale;
+      if (MASKED) {
+        // What a row does not see, and what lies past the last key, has a scale of any kind.
+        const uint32_t see = (uint32_t)(win >> (16 * t + r)) & 1u;
+        y = __uint_as_float(see ? __float_as_uint(y) : 0u);
+      }
+      pf[0][t / 2][t % 2 * 4 + r] = (__bf16)y;
+    }
+  bool grow = sum > kGrow;
+  if (MASKED) grow |= !(w.m[0] > kNoKey4) && (win & 0x000f000f000f000full) != 0;  // a row's first keys, whatever their weights
+  if (__builtin_expect(__ballot(grow) != 0 && !set, 0)) return false;
+  w.l[0] += sum;
+  lds_wait();  // K has been read
+  refill_k();
+  add_products4<1, D>(w, vp, pf);
   return true;
 }
 
 // Folds blocks blk0 .. blk0 + ntiles - 1 (at most 64) of request `lo` of the launch and one KV head
-// into the rows from `row0` on; a ring of N blocks.
-template <int RB, int D, int N>
+// into the rows from `row0` on; a ring of N blocks.  FEW: one row block, and so few blocks that the pass over the first
+// one's scores counts (joined requests 0.3-0.8 us of 8-14 less; in chunks of a long stream 1 % more).
+template <int RB, int D, int N, bool FEW>
 __device__ __forceinline__ void fold_keys(Wave4<RB, D>& w, const AttnShape& s, const AttnBatch& bt, const Kv4Pool& pool,
                                           const uint16_t* __restrict__ q, unsigned char* ring, int lo, int head, int row0,
                                           int blk0, int ntiles) {
@@ -363,9 +435,14 @@ __device__ __forceinline__ void fold_keys(Wave4<RB, D>& w, const AttnShape& s, c
     arrived(t);
     const unsigned char* kp = place(t);
     const bool more = t + N < ntiles;
-    const bool done = fold_block4<RB, D, MASKED>(w, kp, kp + R::kHalf, s.scale_log2, offset(t), t == own, careful, [&] {
+    auto refill_k = [&] {
       if (more) fetch(t + N, false);
-    });
+    };
+    bool done;
+    if constexpr (FEW)
+      done = fold_block_one<D, MASKED>(w, kp, kp + R::kHalf, s.scale_log2, offset(t), t == own, careful, refill_k);
+    else
+      done = fold_block4<RB, D, MASKED>(w, kp, kp + R::kHalf, s.scale_log2, offset(t), t == own, careful, refill_k);
     if (done) {
       lds_wait();
       if (more) fetch(t + N, true);
@@ -373,13 +450,14 @@ __device__ __forceinline__ void fold_keys(Wave4<RB, D>& w, const AttnShape& s, c
     return done;
   };
   int t = 0;
-  if (ntiles > 0) arrived(0);
+  if constexpr (!FEW) {
+    if (ntiles > 0) arrived(0);
+  }
   while (t < ntiles) {
-    careful = set_reference<RB, D>(w, place(t), s.scale_log2, offset(t));
     own = t;
+    if constexpr (!FEW) careful = set_reference<RB, D>(w, place(t), s.scale_log2, offset(t));
     bool done = true;
-    if (!careful)
-      for (; t < whole && done; t += done) done = step(__builtin_amdgcn_readfirstlane(t), Kind<false>());
+    for (; t < whole && done && !careful; t += done) done = step(__builtin_amdgcn_readfirstlane(t), Kind<false>());
     for (; t < ntiles && done; t += done) done = step(__builtin_amdgcn_readfirstlane(t), Kind<true>());
   }
 }
@@ -397,7 +475,7 @@ __device__ __forceinline__ void attend_item(const AttnShape& s, const AttnBatch&
   const int key_begin = (c - __builtin_amdgcn_readlane(prefix, lo)) * s.chunk_keys;
   const int key_end = min(key_begin + s.chunk_keys, bt.kv_len[lo]);
   Wave4<RB, D> w;
-  fold_keys<RB, D, N>(w, s, bt, pool, q, ring, lo, head, row0, key_begin / kKeyBlock4,
+  fold_keys<RB, D, N, false>(w, s, bt, pool, q, ring, lo, head, row0, key_begin / kKeyBlock4,
                       __builtin_amdgcn_readfirstlane((key_end - key_begin + kKeyBlock4 - 1) / kKeyBlock4));
   const int64_t slot = (int64_t)(bt.chunk_base + c) * s.Hkv + head;
 #pragma unroll
@@ -474,7 +552,7 @@ void kv4_attn_join_kernel(AttnShape s, AttnBatch bt, Kv4Pool pool, ByLength orde
   const int from = blocks * wave / W, to = blocks * (wave + 1) / W;
   unsigned char* const mine = ring + wave * kRing;
   Wave4<1, D> w;
-  fold_keys<1, D, N>(w, s, bt, pool, q, mine, lo, head, rg * 16, from, __builtin_amdgcn_readfirstlane(to - from));
+  fold_keys<1, D, N, true>(w, s, bt, pool, q, mine, lo, head, rg * 16, from, __builtin_amdgcn_readfirstlane(to - from));
   lds_wait();
   float* const o = reinterpret_cast<float*>(mine) + lr * kRow + 4 * lg;
 #pragma unroll
