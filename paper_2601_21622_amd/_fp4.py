@@ -26,6 +26,9 @@ SD_KV4_GROUP = 32
 _HEADER = os.path.join(os.path.dirname(_b._HEADER), "sdverify_fp4.h")
 
 
+_SCALES = (torch.bfloat16, torch.int16, torch.uint16)
+
+
 class KV4Cache(ctypes.Structure):
     """sd_kv4_cache_t: a 4-bit paged cache.  Build it with KV4Cache.of(...),
     which checks the pools against each other and keeps them referenced."""
@@ -53,7 +56,7 @@ class KV4Cache(ctypes.Structure):
         keys = pages * heads * page_size
         if any(t.element_size() != 1 for t in (k, v, k_scale)) or v.numel() != k.numel():
             raise ValueError("k, v and k_scale must be bytes, k and v of one size")
-        if v_scale.element_size() != 2 or v_scale.numel() != keys:
+        if v_scale.dtype not in _SCALES or v_scale.numel() != keys:
             raise ValueError("v_scale must be a bfloat16 for each key")
         dim = 2 * k.numel() // max(1, keys)
         if dim * keys != 2 * k.numel() or k_scale.numel() * SD_KV4_GROUP != dim * keys:

@@ -2,24 +2,40 @@
 //
 //   O = softmax(scale * Q K^T + mask) V,  K = code * 2^e of its key's 32 columns, V = code * s of its key.
 //
-// The G * group queries that share a KV head are the rows of one KV head.  One
-// wave, a workgroup of its own, per work item (chunk of whole 64-key blocks of one
-// request, KV head, group of rows); each item writes a partial (reference maximum, sum, O)
-// and the merge joins them in chunk order.
+// The G * group queries that share a KV head are the rows of one KV head, in blocks of 16.  Two ways:
+//  * In chunks: one wave, a workgroup of its own, per work item (chunk of whole 64-key
+//    blocks of one request, KV head, group of up to five row blocks); each item writes a partial
+//    (reference maximum, sum, O) and the merge joins them in chunk order.
+//  * Joined: a workgroup of eight waves takes a whole request, KV head and row block, and joins its
+//    waves' O in LDS: where requests are short, one launch and no partials.
+// Which way, and how long a chunk is, kv4_shape decides by what either takes.
+//
+// What bounds it: with one row block the caches' stream, 6.0-6.1 TB/s on long chunks (4 x 200,000 keys, 8 KV
+// heads, D = 128, 857 MB: 140 us with the merge) and 5.2 where items are short (64 pooled requests of 128-8,192 keys, 32
+// heads, 547 MB: kernel 104 us, of which about 15 are the first blocks' arrival and the last items' end).  With more
+// row blocks a wave's own instructions: of 72 rows (five blocks) 16 x 16,384-32,768 keys take 155 us, where the
+// products alone are 83-96 at a large library product's rate and the stream 70.  A wave issues an instruction about every five cycles,
+// a product hides two vector instructions, an exponential takes eight cycles, a widening four and a half; 917
+// instructions fold 64 keys into 80 rows.  Five row blocks in one wave beat three and two in two (165 and 190 us the
+// whole call): keys are widened once, and two waves drift apart until the second reads the caches again from memory
+// (820 MB instead of 415).
 //
 // A K fragment is what a lane loads: 8 codes of one key, whose scale the widening
 // instruction takes.  V lies key by key, so that an append writes rows, and is transposed on
 // its way out of LDS: a lane gets one column of the 16 keys whose scores it holds
 // (S^T = K Q^T; tile t: keys 16 t + 4 g + r of group g = lane / 16), which is all that
 // O^T += V^T P^T needs.  V's scale multiplies the weight, in float32, before the weight
-// is rounded to bfloat16 for the product with V's codes.
+// is rounded to bfloat16 for the product with V's codes (half a step: 2^-8 of each term; bfloat16 for its
+// range, which a product with a scale needs).  The 4-bit matrix instructions would take K without widening, but keep
+// too few bits of their sums: 6.6e-5 of the sum of magnitudes of 128 products, measured.
 //
 // Softmax in the log2 domain, against a reference that is the row's maximum as of the
-// last time it was set: scores may pass it by 2^8 before O is rescaled, which a wave
-// notices by the sums that it keeps anyway.  Accumulators start at -reference.  Where a
-// reference is so large that sums that start there round differently from those that start
-// at zero by more than a 2^8th (kCareful), and in the block that sets it, scores are summed
-// from zero and the reference is subtracted from the sum.
+// last time it was set: a lane's weights of a block may sum to 2^8 before the reference is set again and O
+// rescaled, which a wave notices by the sums that it keeps anyway.  That happens outside the loop over the blocks:
+// inside, the compiler spills O, and a spill's reload waits for the DMAs before it.  Accumulators start
+// at -reference.  Where a reference is large (2^16 in the log2 domain: sums that start there round differently from those that
+// start at zero, by up to 2^-8 and, further up, by any factor), and for the block that sets it, scores are summed
+// from zero and the reference is subtracted from the sum: equal scores stay equal, and none exceeds its own maximum.
 #include <algorithm>
 
 #include "fp4.h"
@@ -30,8 +46,10 @@ namespace sdv {
 
 namespace {
 
-constexpr int kMaxTiles4 = 64;  // blocks per chunk: one lane holds one block's page
-constexpr int kJoinWaves = 8;     // of a workgroup that takes a request; 16 on rings of one block: 9.8 us where 8 take 8.9 (1,000 keys, one token)
+constexpr int kMaxTiles4 = 64;   // blocks per chunk: one lane holds one block's page
+// Waves of a workgroup that takes a request.  Sixteen, on rings of one block: 9.8 us where eight take 8.9 (1,000
+// keys, one token, D = 128), 14.2 and 12.5 (4 x 1,500 keys, 72 rows).
+constexpr int kJoinWaves = 8;
 constexpr int kManyChunks = 16;  // chunks of a request that one thread joins
 constexpr float kNoKey4 = -3.402823466e38f;  // reference of a row that has seen no key: no score lies below it
 constexpr float kGrow = 256.f;      // sum of a lane's 16 weights of a block that sets a new reference
@@ -581,7 +599,12 @@ void kv4_attn_join_kernel(AttnShape s, AttnBatch bt, Kv4Pool pool, ByLength orde
   }
 }
 
-// 16-row blocks of a wave, at most; more rows are split over row groups, a wave each.
+// 16-row blocks of a wave, at most; more rows are split over row groups, a wave each.  `blocks`: 64-key
+// blocks times heads.  Where the caches are few blocks per CU, what counts is how long a wave takes for its own; where they are
+// many, that keys are read and widened once.  8 heads, requests of one length, us with at most 1, 2 and 5 row blocks:
+//   D = 128, 72 rows: 4 x 1,500 keys (750 blocks) 15.8, 17.8, 29.6; 64 x 1,500 (12,300) 88, 75, 66; 16 x 24,576 281, 221, 182
+//            40 rows: 24 x 1,400 (4,200) 27.9, 31.7, 36.5;  128 rows: 8 x 9,000 (9,000) 70.5, 64.9, 69.5
+//   D = 64:  48 rows: 13 x 1,500 (2,500) 16.5, 17.5, 19.9;  128 rows: 8 x 9,000 55.0, 48.3, 49.2;  72 rows: 16 x 24,576 152, 141, 126
 int max_blocks4(int64_t blocks) { return blocks <= 24 * cu_count() ? 1 : blocks <= 40 * cu_count() ? 2 : 5; }
 int blocks_of4(int rows, int groups) { return ((rows + 15) / 16 + groups - 1) / groups; }
 

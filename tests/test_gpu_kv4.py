@@ -464,14 +464,15 @@ def test_attention_of_large_and_small_values(exponent, D):
     check_attention(got, q.double().numpy(), c.segments(lens), lens, Hkv, None, 1 / np.sqrt(D), str(exponent))
 
 
-def test_streams_graphs_and_workspaces():
+@pytest.mark.parametrize("lens", [[133, 700, 64], [2500, 9000, 64]], ids=["joined", "chunks"])
+def test_streams_graphs_and_workspaces(lens):
     """A captured step (append, attention) replayed over changing inputs, with eager work between the
     replays and calls on another stream with a workspace of their own; results do not depend on either."""
     rng = np.random.default_rng(15)
-    G, Hq, Hkv, D, lens = 5, 8, 4, 128, [133, 700, 64]
+    G, Hq, Hkv, D = 5, 8, 4, 128
     c = filled(rng, lens, Hkv, D, 64)
     d = sd.Dims(3, G - 1, Hq, Hkv, D, 32, 1, 1, 0)
-    n = sd.sd_kv4_workspace_bytes(d, 1000)
+    n = sd.sd_kv4_workspace_bytes(d, max(lens))
     ws, ws2 = (torch.empty(n, dtype=torch.uint8, device="cuda") for _ in range(2))
     q = torch.zeros((3, G, Hq, D), dtype=torch.bfloat16, device="cuda")
     k_new, v_new = (torch.zeros((3 * G, Hkv, D), dtype=torch.bfloat16, device="cuda") for _ in range(2))
@@ -653,7 +654,7 @@ def test_binding_refuses_what_does_not_fit():
         sd.sd_verify_attention_kv4(d, t, c.handle, [64], None, 0.1, t, torch.zeros(16, dtype=torch.uint8, device="cuda"))
     pools = [*c.dev[:3], c.dev[3].view(torch.bfloat16), torch.zeros((1, 1), dtype=torch.int32, device="cuda")]
     for i, bad in ((0, pools[0][:1]), (1, pools[1][..., :100].contiguous()), (2, pools[2][..., :64].contiguous()),
-                   (3, pools[3].float()), (4, pools[4].long())):
+                   (3, pools[3].float()), (3, pools[3].half()), (4, pools[4].long())):
         with pytest.raises(ValueError):
             sd.KV4Cache.of(*pools[:i], bad, *pools[i + 1:], 64)
     with pytest.raises(ValueError):
