@@ -110,7 +110,7 @@ def exported_fp8_symbols() -> list:
 
 def _device(tensors) -> int:
     """The index of the one device of the tensors (None among them is left out)."""
-    dev = -1
+    dev = -2  # none yet; a host tensor's is -1
     for t in tensors:
         if t is None:
             continue

@@ -8,6 +8,7 @@ import pytest
 import torch
 
 import paper_2601_21622_amd as sd
+from paper_2601_21622_amd import _fp8
 
 P = 0x100000  # a fake, aligned address: every call below fails its host checks
 cpu_only = pytest.mark.skipif(torch.cuda.is_available(), reason="host-validation tests use fake pointers")
@@ -158,3 +159,25 @@ def test_binding_refuses_host_tensors():
         sd.sd_qk_norm_rope(t.numpy(), t, t, t, None, None, 1e-6, t, t)
     with pytest.raises(ValueError):
         sd.KV4Cache.of(t, t, t, t, torch.zeros(1, 1, dtype=torch.int32), 64)
+
+
+class _OnGpu(torch.Tensor):
+    """A tensor that says it lies on the first GPU."""
+
+    def get_device(self):
+        return 0
+
+
+@pytest.mark.parametrize("order", ["host", "host first", "host last"])
+def test_one_host_tensor_is_refused(order):
+    host, gpu = torch.zeros(8), torch.zeros(8).as_subclass(_OnGpu)
+    tensors = {"host": [host, None, host], "host first": [None, host, gpu], "host last": [gpu, None, host]}[order]
+    with pytest.raises(ValueError, match="GPU tensors"):
+        _fp8._device(tensors)
+    assert _fp8._device([None, gpu, gpu]) == 0
+
+
+def test_binding_refuses_well_formed_host_tensors():
+    q, f, pos = torch.zeros(4, 2, 64), torch.zeros(32), torch.zeros(4, dtype=torch.int32)
+    with pytest.raises(ValueError, match="GPU tensors"):
+        sd.sd_qk_norm_rope(q, q, pos, f, None, None, 1e-6, q, q)
