@@ -152,8 +152,8 @@ def _lengths(a, dtype, batch: int, what: str):
 
 def _passes(off, count, limit: int) -> bool:
     """Whether some request's rows end past `limit` (a request without rows has none)."""
-    end = off + count
-    return end.max() > limit and bool(((end > limit) & (count > 0)).any())
+    over = off > np.subtract(limit, count, dtype=np.int64)  # a sum could wrap
+    return bool(over.any()) and bool((over & (count > 0)).any())
 
 
 def _run(fn, where: str, dev: int, stream, *args) -> None:

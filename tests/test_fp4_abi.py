@@ -4,6 +4,7 @@ only tensors show."""
 
 import ctypes
 
+import numpy as np
 import pytest
 import torch
 
@@ -181,3 +182,11 @@ def test_binding_refuses_well_formed_host_tensors():
     q, f, pos = torch.zeros(4, 2, 64), torch.zeros(32), torch.zeros(4, dtype=torch.int32)
     with pytest.raises(ValueError, match="GPU tensors"):
         sd.sd_qk_norm_rope(q, q, pos, f, None, None, 1e-6, q, q)
+
+
+@pytest.mark.parametrize("off,count,over", [
+    ([0, 6], [4, 4], False), ([0, 7], [4, 4], True), ([0, 99], [10, 0], False), ([0, 0], [11, 0], True), ([10], [0], False),
+    ([2 ** 63 - 1], [1], True), ([2 ** 63 - 1], [2 ** 31 - 1], True), ([2 ** 63 - 1], [0], False), ([0], [-2 ** 31], False)])
+def test_rows_past_the_last_are_noticed(off, count, over):
+    """Negative counts and offsets are the call's own to refuse; sums do not wrap."""
+    assert _fp8._passes(np.array(off), np.array(count, dtype=np.int32), 10) == over
