@@ -73,15 +73,15 @@ __device__ __forceinline__ void half_dma(const void* codes, uint32_t off16, uint
   if (D == 128)
     asm volatile(
         "s_mov_b32 m0, %1\n\ts_mov_b64 %0, %3\n\tglobal_load_lds_dwordx4 %2, %0 nt\n\t"
-        "global_load_lds_dwordx4 %2, %0 offset:1024 nt\n\tglobal_load_lds_dwordx4 %2, %0 offset:2048 nt\n\t"
-        "global_load_lds_dwordx4 %2, %0 offset:3072 nt"
+        "global_load_lds_dwordx4 %2, %0 offset:0x400 nt\n\tglobal_load_lds_dwordx4 %2, %0 offset:0x800 nt\n\t"
+        "global_load_lds_dwordx4 %2, %0 offset:0xc00 nt"
         : "=&s"(from)
         : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(off16), "s"(codes)
         : "m0", "memory");
   else
     asm volatile(
         "s_mov_b32 m0, %1\n\ts_mov_b64 %0, %3\n\tglobal_load_lds_dwordx4 %2, %0 nt\n\t"
-        "global_load_lds_dwordx4 %2, %0 offset:1024 nt"
+        "global_load_lds_dwordx4 %2, %0 offset:0x400 nt"
         : "=&s"(from)
         : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(off16), "s"(codes)
         : "m0", "memory");
