@@ -11,14 +11,14 @@
 // Which way, and how long a chunk is, kv4_shape decides by what either takes.
 //
 // What bounds it: with one row block the caches' stream, 6.0-6.1 TB/s on long chunks (4 x 200,000 keys, 8 KV
-// heads, D = 128, 857 MB: 140 us with the merge) and 5.2 where items are short (64 pooled requests of 128-8,192 keys, 32
-// heads, 547 MB: kernel 104 us, of which about 15 are the first blocks' arrival and the last items' end).  With more
-// row blocks a wave's own instructions: of 72 rows (five blocks) 16 x 16,384-32,768 keys take 155 us, where the
-// products alone are 83-96 at a large library product's rate and the stream 70.  A wave issues an instruction about every five cycles,
-// a product hides two vector instructions, an exponential takes eight cycles, a widening four and a half; 917
-// instructions fold 64 keys into 80 rows.  Five row blocks in one wave beat three and two in two (165 and 190 us the
-// whole call): keys are widened once, and two waves drift apart until the second reads the caches again from memory
-// (820 MB instead of 415).
+// heads, D = 128, 857 MB: 140 us with the merge) and 5.2 where items are short (64 pooled requests of
+// 128-8,192 keys, 32 heads, 547 MB: kernel 103-107 us).  With more row blocks a wave's own instructions: of
+// 72 rows (five blocks) 16 x 16,384-32,768 keys take 154-162 us, where the products alone are 83-96 at a
+// large library product's rate and the stream 70.  A wave issues an instruction about every five cycles, a
+// product hides two vector instructions, an exponential takes eight cycles, a widening four and a half; 917
+// instructions fold 64 keys into 80 rows.  Five row blocks in one wave beat three and two in two (165 and 190
+// us the whole call): keys are widened once, and two waves drift apart until the second reads the caches
+// again from memory (820 MB instead of 415).
 //
 // A K fragment is what a lane loads: 8 codes of one key, whose scale the widening
 // instruction takes.  V lies key by key, so that an append writes rows, and is transposed on
