@@ -196,7 +196,9 @@ __device__ __forceinline__ void decode8(uint32_t codes, float scale, float (&x)[
   decode2<3>(codes, scale, x);
 }
 
-template <typename T, int D>
+// K and V: which of them are asked for.  8 sessions of 1 to 9,001 keys, 8 heads, D = 128, us: both 40, one of them
+// 19 (24-25 where the other's codes are read too); chosen at run time, by branches among the loads, 45 and 22.
+template <typename T, int D, bool K, bool V>
 __global__ __launch_bounds__(kRowThreads)
 void kv4_read_kernel(Kv4Rows rows, Kv4Pool pool, int Hkv, int nunits, T* __restrict__ k_out, int64_t k_stride,
                      T* __restrict__ v_out, int64_t v_stride) {
@@ -215,18 +217,21 @@ void kv4_read_kernel(Kv4Rows rows, Kv4Pool pool, int Hkv, int nunits, T* __restr
   const uint8_t* const v_in = pool.v + t.block * (32 * D) + t.key0 * 8;
   const uint8_t* const k_scale = pool.k_scale + t.block * (2 * D) + t.key0 / kTile;
   const uint16_t* const v_scale = pool.v_scale + t.block * kKeyBlock4 + t.key0;
-  float ks[kRounds], vs[kRounds];
+  [[maybe_unused]] float ks[kRounds], vs[kRounds];
 #pragma unroll
   for (int i = 0; i < kRounds; ++i) {
     const int key = i * kKeys + lane / TPR;
-    ks[i] = __uint_as_float((uint32_t)k_scale[(col / kGroup4 * 16 + key) * 4] << 23);
-    vs[i] = bf16_to_f32(v_scale[key]);
+    if constexpr (K) ks[i] = __uint_as_float((uint32_t)k_scale[(col / kGroup4 * 16 + key) * 4] << 23);
+    if constexpr (V) vs[i] = bf16_to_f32(v_scale[key]);
   }
-  if (D == 128)
-    reinterpret_cast<u32x4*>(k_image)[lane] = reinterpret_cast<const u32x4*>(k_in)[lane];
-  else
-    reinterpret_cast<u32x2*>(k_image)[lane] = reinterpret_cast<const u32x2*>(k_in)[lane];
-  if (lane < D / 2) reinterpret_cast<u32x4*>(v_image)[lane] = *reinterpret_cast<const u32x4*>(v_in + lane / 8 * 512 + lane % 8 * 16);
+  if constexpr (K) {
+    if (D == 128)
+      reinterpret_cast<u32x4*>(k_image)[lane] = reinterpret_cast<const u32x4*>(k_in)[lane];
+    else
+      reinterpret_cast<u32x2*>(k_image)[lane] = reinterpret_cast<const u32x2*>(k_in)[lane];
+  }
+  if (V && lane < D / 2)
+    reinterpret_cast<u32x4*>(v_image)[lane] = *reinterpret_cast<const u32x4*>(v_in + lane / 8 * 512 + lane % 8 * 16);
   lds_wait();
 #pragma unroll
   for (int i = 0; i < kRounds; ++i) {
@@ -235,12 +240,16 @@ void kv4_read_kernel(Kv4Rows rows, Kv4Pool pool, int Hkv, int nunits, T* __restr
     const int64_t row = t.row0 + key;
     if (i * kKeys >= t.to || (i + 1) * kKeys <= t.from) continue;
     float x[8];
-    decode8(k_image[k_dword<D>(key, col)], ks[i], x);
-    if (mine && k_out != nullptr) store_row8(k_out + row * k_stride + t.head * D + col, x);
-    decode8(v_image[v_dword(key, col)], 1.f, x);
+    if constexpr (K) {
+      decode8(k_image[k_dword<D>(key, col)], ks[i], x);
+      if (mine) store_row8(k_out + row * k_stride + t.head * D + col, x);
+    }
+    if constexpr (V) {
+      decode8(v_image[v_dword(key, col)], 1.f, x);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] *= vs[i];
-    if (mine && v_out != nullptr) store_row8(v_out + row * v_stride + t.head * D + col, x);
+      for (int e = 0; e < 8; ++e) x[e] *= vs[i];
+      if (mine) store_row8(v_out + row * v_stride + t.head * D + col, x);
+    }
   }
 }
 
@@ -270,9 +279,17 @@ hipError_t launch_kv4_read(const Kv4Rows& r, const Kv4Pool& pool, int Hkv, int D
                            int64_t k_stride, void* v_out, int64_t v_stride, hipStream_t stream) {
   const int nunits = r.prefix[r.nreq] * Hkv;
   const dim3 grid((nunits + kRowThreads / kWave - 1) / (kRowThreads / kWave)), block(kRowThreads);
-#define SDV_READ(T, DIM)                                                                                         \
-  hipLaunchKernelGGL((kv4_read_kernel<T, DIM>), grid, block, 0, stream, r, pool, Hkv, nunits,                    \
+#define SDV_READ_OF(T, DIM, K, V)                                                                                \
+  hipLaunchKernelGGL((kv4_read_kernel<T, DIM, K, V>), grid, block, 0, stream, r, pool, Hkv, nunits,              \
                      static_cast<T*>(k_out), k_stride, static_cast<T*>(v_out), v_stride)
+#define SDV_READ(T, DIM)                  \
+  if (k_out != nullptr && v_out != nullptr) { \
+    SDV_READ_OF(T, DIM, true, true);      \
+  } else if (k_out != nullptr) {          \
+    SDV_READ_OF(T, DIM, true, false);     \
+  } else {                                \
+    SDV_READ_OF(T, DIM, false, true);     \
+  }
   if (f32 && D == 128) {
     SDV_READ(float, 128);
   } else if (f32) {
@@ -283,6 +300,7 @@ hipError_t launch_kv4_read(const Kv4Rows& r, const Kv4Pool& pool, int Hkv, int D
     SDV_READ(uint16_t, 64);
   }
 #undef SDV_READ
+#undef SDV_READ_OF
   return hipGetLastError();
 }
 
