@@ -31,7 +31,7 @@ _SCALES = (torch.bfloat16, torch.int16, torch.uint16)
 
 class KV4Cache(ctypes.Structure):
     """sd_kv4_cache_t: a 4-bit paged cache.  Build it with KV4Cache.of(...),
-    which checks the pools against each other and keeps them referenced."""
+    which checks the pools against each other and keeps them referenced as long as it lives."""
     _fields_ = [
         ("k", ctypes.c_void_p),
         ("v", ctypes.c_void_p),
@@ -67,7 +67,6 @@ class KV4Cache(ctypes.Structure):
         c._tensors = (k, v, k_scale, v_scale, block_table)
         c._heads, c._dim, c._rows = heads, dim, int(block_table.shape[0])
         c._device = _device(c._tensors)
-        c._ref = ctypes.byref(c)
         return c
 
     def _fits(self, dims: Dims, dev: int) -> None:
@@ -171,7 +170,7 @@ def sd_kv4_append(dims: Dims, cache: KV4Cache, k_new, v_new, new_off: Sequence[i
         raise ValueError("new_off + new_len passes the last new row")
     if (k == 0 or v == 0) and not (new > 0).any():  # no rows at all: nothing to append
         return
-    _run(_library().sd_kv4_append, "sd_kv4_append", dev, stream, ctypes.byref(dims), cache._ref, k, k_stride,
+    _run(_library().sd_kv4_append, "sd_kv4_append", dev, stream, ctypes.byref(dims), ctypes.byref(cache), k, k_stride,
          v, v_stride, off_p, new_p, len_p)
 
 
@@ -190,8 +189,8 @@ def sd_kv4_read(dims: Dims, cache: KV4Cache, first: Sequence[int], count: Sequen
         raise ValueError("out_off + count passes the last row")
     if not (k or v) and not (n > 0).any():  # no rows at all: nothing to read
         return
-    _run(_library().sd_kv4_read, "sd_kv4_read", dev, stream, ctypes.byref(dims), cache._ref, at_p, n_p, off_p, k, k_stride,
-         v, v_stride)
+    _run(_library().sd_kv4_read, "sd_kv4_read", dev, stream, ctypes.byref(dims), ctypes.byref(cache), at_p, n_p,
+         off_p, k, k_stride, v, v_stride)
 
 
 def sd_verify_attention_kv4(dims: Dims, q, cache: KV4Cache, kv_len: Sequence[int], parent, scale: float, out, workspace,
@@ -202,5 +201,5 @@ def sd_verify_attention_kv4(dims: Dims, q, cache: KV4Cache, kv_len: Sequence[int
     ln, len_p = _lengths(kv_len, np.int32, dims.batch, "kv_len")
     p = None if parent is None else _typed(parent, torch.int32, "parent", dims.batch * dims.gamma)
     _run(_library().sd_verify_attention_kv4, "sd_verify_attention_kv4", dev, stream, ctypes.byref(dims),
-         _typed(q, torch.bfloat16, "q", n), cache._ref, len_p, p, float(scale),
+         _typed(q, torch.bfloat16, "q", n), ctypes.byref(cache), len_p, p, float(scale),
          _typed(out, torch.bfloat16, "out", n), _b._ptr(workspace), _b._nbytes(workspace))

@@ -28,7 +28,7 @@ _TYPES = {SD_DTYPE_F32: torch.float32, SD_DTYPE_BF16: torch.bfloat16}
 
 class KV8Cache(ctypes.Structure):
     """sd_kv8_cache_t: an 8-bit paged cache.  Build it with KV8Cache.of(...),
-    which checks the pools against each other and keeps them referenced."""
+    which checks the pools against each other and keeps them referenced as long as it lives."""
     _fields_ = [
         ("k", ctypes.c_void_p),
         ("v", ctypes.c_void_p),
@@ -64,7 +64,6 @@ class KV8Cache(ctypes.Structure):
         if c._dim * rows != k.numel():
             raise ValueError("a pool's size is not pages * heads * page_size * head_dim")
         c._device = _device(c._tensors)
-        c._ref = ctypes.byref(c)
         return c
 
     def _fits(self, dims: Dims, dev: int) -> None:
@@ -206,7 +205,7 @@ def sd_kv8_append(dims: Dims, cache: KV8Cache, k_new, v_new, new_off: Sequence[i
     if k == 0 or v == 0:  # no rows at all: nothing to append
         if k_new.numel() == 0 and v_new.numel() == 0 and not (new > 0).any():
             return
-    _run(_library().sd_kv8_append, "sd_kv8_append", dev, stream, ctypes.byref(dims), cache._ref, k, k_stride,
+    _run(_library().sd_kv8_append, "sd_kv8_append", dev, stream, ctypes.byref(dims), ctypes.byref(cache), k, k_stride,
          v, v_stride, off_p, new_p, len_p)
 
 
@@ -218,7 +217,7 @@ def sd_verify_attention_kv8(dims: Dims, q, cache: KV8Cache, kv_len: Sequence[int
     ln, len_p = _lengths(kv_len, np.int32, dims.batch, "kv_len")
     p = None if parent is None else _typed(parent, torch.int32, "parent", dims.batch * dims.gamma)
     _run(_library().sd_verify_attention_kv8, "sd_verify_attention_kv8", dev, stream, ctypes.byref(dims),
-         _typed(q, torch.bfloat16, "q", n), cache._ref, len_p, p, float(scale),
+         _typed(q, torch.bfloat16, "q", n), ctypes.byref(cache), len_p, p, float(scale),
          _typed(out, torch.bfloat16, "out", n), _b._ptr(workspace), _b._nbytes(workspace))
 
 
