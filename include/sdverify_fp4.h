@@ -120,7 +120,10 @@ SD_API int sd_qk_norm_rope(const sd_rope_t* rope, const void* q, int64_t q_strid
  * With x the largest magnitude of a key's 32 columns, their scale is the smallest
  * 2^e >= 2^-100 with x <= 6 * 2^e; with x that of a value's row, its scale is the
  * smallest bfloat16 s >= 2^-100 with x <= 6 s.  Codes are nearest to the element
- * over its scale, ties to the even code; nothing saturates.  Columns of a scale with an
+ * over its scale, ties to the even code.  The largest scales are those with which 6
+ * is finite in float32, 2^125 and 170 * 2^118: elements past 6 * 2^125 = 1.5 * 2^127
+ * (of values, past bfloat16's largest number) become that; nothing else saturates,
+ * and what is finite stays finite.  Columns of a scale with an
  * infinity or NaN among them become NaN, all of them (scale byte 255, scale 0x7fc0,
  * codes 0).  Other keys' bytes are not touched.  The keys that a call writes
  * belong to one request each; calls on one cache run one after another.

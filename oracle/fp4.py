@@ -17,6 +17,9 @@ import numpy as np
 BLOCK = 64
 GROUP = 32
 LOWEST = -100
+# The largest scales with which 6, the largest code, stands for a finite float32: 2^125, and the bits of 170 * 2^118.
+HIGHEST = 125
+HIGHEST_VALUE = 0x7e2a
 VALUES = np.array([0, 0.5, 1, 1.5, 2, 3, 4, 6, -0.0, -0.5, -1, -1.5, -2, -3, -4, -6])
 
 
@@ -108,7 +111,7 @@ def rows(k, v, k_scale, v_scale, table_row, first, count, head):
 
 def append(k, v, k_scale, v_scale, table, k_new, v_new, new_off, new_len, kv_len):
     """The four pools after an append (copies).  New rows [T][Hkv][D]; request b's keys
-    kv_len - new_len .. are its rows new_off .. ."""
+    kv_len - new_len .. are its rows new_off .. .  Elements past 6 of the largest scale become 6 of it."""
     k, v, k_scale, v_scale = k.copy(), v.copy(), k_scale.copy(), v_scale.copy()
     heads, blocks, dim = k.shape[1], k.shape[2], k.shape[3] // 32
     ki, vi, si = k_index(dim), v_index(dim), k_scale_index(dim)
@@ -121,13 +124,13 @@ def append(k, v, k_scale, v_scale, table, k_new, v_new, new_off, new_len, kv_len
                 codes = unpack(k[at])
                 for g in range(dim // GROUP):
                     number = np.isfinite(x[g]).all()
-                    e = scale_exponent(np.abs(x[g]).max()) if number else 128
+                    e = min(scale_exponent(np.abs(x[g]).max()), HIGHEST) if number else 128
                     codes[ki[n % BLOCK, g * GROUP:(g + 1) * GROUP]] = encode(x[g] * 2.0 ** -e) if number else 0
                     k_scale[at][si[n % BLOCK, g]] = e + 127
                 k[at] = pack(codes)
                 x = np.asarray(v_new[int(new_off[b]) + j, h], dtype=np.float64)
                 number = np.isfinite(x).all()
-                s = value_scale(np.abs(x).max()) if number else 0x7fc0
+                s = min(value_scale(np.abs(x).max()), HIGHEST_VALUE) if number else 0x7fc0
                 codes = unpack(v[at])
                 # float64 quotients of float32 by bfloat16 fall on a border of codes only where the true ones do
                 codes[vi[n % BLOCK]] = encode(x / bf16_value(s)) if number else 0

@@ -20,6 +20,10 @@ namespace {
 
 constexpr int kRowThreads = 256;
 constexpr int kLowestExp4 = 27;  // byte of the smallest scale, 2^-100
+// Largest scales with which 6 stands for a finite float32: 2^125 of keys, by its byte, and 170 * 2^118 of values (6 of it is
+// bfloat16's largest number).  With the next ones finite rows would come back infinite; elements past 6 of them become 6.
+constexpr int kHighestExp4 = 252;
+constexpr float kHighestScale4 = 0x1.54p125f;
 constexpr uint32_t kInfBits = 0x7f800000u;
 
 // A wave's tile.
@@ -73,19 +77,19 @@ __device__ __forceinline__ uint32_t row_max(uint32_t v) {
   return D == 128 ? max(v, dpp_u32<kDppRowMirror>(v)) : v;
 }
 
-// Smallest exponent byte, at least 27, with x <= 6 * 2^(byte - 127); x by its bits.
+// Smallest exponent byte, 27 to 252, with x <= 6 * 2^(byte - 127); x by its bits.
 // 6 = 1.5 * 2^2.
 __device__ __forceinline__ int key_scale(uint32_t x) {
-  return max((int)(x >> 23) - 2 + ((x & 0x7fffffu) > 0x400000u ? 1 : 0), kLowestExp4);
+  return min(max((int)(x >> 23) - 2 + ((x & 0x7fffffu) > 0x400000u ? 1 : 0), kLowestExp4), kHighestExp4);
 }
 
-// Smallest bfloat16 s, at least 2^-100, with x <= 6 s (6 s is exact).  The product with
+// Smallest bfloat16 s, 2^-100 to 170 * 2^118, with x <= 6 s (6 s is exact).  The product with
 // 1/6 is off by less than a bfloat16 step, so that the truncated one is at most two below.
 __device__ __forceinline__ float value_scale(float x) {
   uint32_t b = __float_as_uint(x * (1.f / 6.f)) & 0xffff0000u;
 #pragma unroll
   for (int i = 0; i < 2; ++i) b += 6.f * __uint_as_float(b) < x ? 0x10000u : 0u;
-  return fmaxf(__uint_as_float(b), 0x1p-100f);
+  return fminf(fmaxf(__uint_as_float(b), 0x1p-100f), kHighestScale4);
 }
 
 // x / s for the code's rounding: the quotient rounded, which is exact where the true one
