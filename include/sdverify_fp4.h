@@ -159,7 +159,7 @@ SD_API int sd_kv4_read(const sd_dims_t* dims, const sd_kv4_cache_t* cache, const
  *            After acceptance, append the accepted nodes' rows again, from
  *            key kv_len - gamma on, gathered from those that the caller kept: that
  *            is the cache's commit
- *   scale    softmax scale, finite and > 0
+ *   scale    softmax scale, > 0; scale * log2 e is finite in float32
  * G * (n_q_heads / n_kv_heads) <= 128.  Products are exact in float32 and summed
  * there; the weights exp(score - maximum) times the value's scale are rounded to
  * bfloat16 where they multiply V's codes.  Keys that a position does not see

@@ -114,7 +114,7 @@ SD_API int sd_kv8_append(const sd_dims_t* dims, const sd_kv8_cache_t* cache, con
  *            After acceptance, append the accepted nodes' rows again, from
  *            key kv_len - gamma on: that is the cache's commit.  Their rows, which the
  *            caller kept, have to be gathered first: an append takes consecutive rows.
- *   scale    softmax scale, finite and > 0
+ *   scale    softmax scale, > 0; scale * log2 e is finite in float32
  * G * (n_q_heads / n_kv_heads) <= 128.  Keys that a position does not see
  * contribute nothing, whatever they hold; a NaN that it sees makes its output NaN.
  * Scores, and the sum of |V| over a request's keys, have to lie within float32's

@@ -4,6 +4,9 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <cmath>
+
+#include "common.h"
 #include "launch.h"
 #include "sdverify.h"
 
@@ -33,6 +36,9 @@ inline int check_attention(const sd_dims_t* d) {
   if (int64_t(d->gamma + 1) * (d->n_q_heads / d->n_kv_heads) > kMaxRows) return SD_ERR_UNSUPPORTED;
   return SD_OK;
 }
+
+// The kernels work with scale * log2 e.
+inline bool scale_ok(float scale) { return scale > 0.f && std::isfinite(scale * kLog2e); }
 
 inline size_t attention_ws(const AttnShape& s, int64_t chunks) {
   return align_up(attn_partial_bytes(chunks, s.Hkv, s.rows, s.D));

@@ -126,7 +126,7 @@ int sd_verify_attention_kv8(const sd_dims_t* d, const void* q, const sd_kv8_cach
   if (!q || !kv_len || !out || !workspace) return SD_ERR_INVALID_ARGUMENT;
   if (!aligned(q, 16) || !aligned(out, 16) || !aligned(workspace, 16) || (parent != nullptr && !aligned(parent, 4)))
     return SD_ERR_INVALID_ARGUMENT;
-  if (!(scale > 0.f) || !std::isfinite(scale)) return SD_ERR_INVALID_ARGUMENT;
+  if (!scale_ok(scale)) return SD_ERR_INVALID_ARGUMENT;
   const int G = d->gamma + 1;
   for (int b = 0; b < d->batch; ++b)
     if (kv_len[b] < G || !length_ok(cache, kv_len[b])) return SD_ERR_INVALID_ARGUMENT;
