@@ -161,11 +161,13 @@ SD_API int sd_kv4_read(const sd_dims_t* dims, const sd_kv4_cache_t* cache, const
  *            is the cache's commit
  *   scale    softmax scale, > 0; scale * log2 e is finite in float32
  * G * (n_q_heads / n_kv_heads) <= 128.  Products are exact in float32 and summed
- * there; the weights exp(score - maximum) times the value's scale are rounded to
- * bfloat16 where they multiply V's codes.  Keys that a position does not see
+ * there; the weights exp(score - maximum) times the value's scale multiply V's codes
+ * as the sum of two bfloat16 numbers (to 2^-16 of a term), or, where a wave holds more than
+ * 16 query rows (more than 16 rows of a KV head over many keys), as one (2^-8).
+ * Keys that a position does not see
  * contribute nothing, whatever they hold; a NaN that it sees makes its output NaN.
- * Scores, and 512 times the sum of |V| over a request's keys, have to lie within
- * float32's range: what passes it comes out as an infinity or NaN.
+ * Products q k, scores, and 512 times the sum of |V| over a request's keys, have to lie
+ * within float32's range: what passes it comes out as an infinity or NaN.
  */
 SD_API int sd_verify_attention_kv4(const sd_dims_t* dims, const void* q, const sd_kv4_cache_t* cache,
                                    const int32_t* kv_len, const int32_t* parent, float scale, void* out,

@@ -12,8 +12,8 @@
 //
 // What bounds it: with one row block the caches' stream, 6.0-6.1 TB/s on long chunks (4 x 200,000 keys, 8 KV
 // heads, D = 128, 857 MB: 140 us with the merge) and 5.2 where items are short (64 pooled requests of
-// 128-8,192 keys, 32 heads, 547 MB: kernel 103-107 us).  With more row blocks a wave's own instructions: of
-// 72 rows (five blocks) 16 x 16,384-32,768 keys take 154-162 us, where the products alone are 83-96 at a
+// 128-8,192 keys, 32 heads, 547 MB: kernel 105-109 us).  With more row blocks a wave's own instructions: of
+// 72 rows (five blocks) 16 x 16,384-32,768 keys take 154-168 us, where the products alone are 83-96 at a
 // large library product's rate and the stream 70.  A wave issues an instruction about every five cycles, a
 // product hides two vector instructions, an exponential takes eight cycles, a widening four and a half; 917
 // instructions fold 64 keys into 80 rows.  Five row blocks in one wave beat three and two in two (165 and 190
@@ -24,9 +24,15 @@
 // instruction takes.  V lies key by key, so that an append writes rows, and is transposed on
 // its way out of LDS: a lane gets one column of the 16 keys whose scores it holds
 // (S^T = K Q^T; tile t: keys 16 t + 4 g + r of group g = lane / 16), which is all that
-// O^T += V^T P^T needs.  V's scale multiplies the weight, in float32, before the weight
-// is rounded to bfloat16 for the product with V's codes (half a step: 2^-8 of each term; bfloat16 for its
-// range, which a product with a scale needs).  The 4-bit matrix instructions would take K without widening, but keep
+// O^T += V^T P^T needs.  V's scale multiplies the weight, in float32; for the product with V's codes the weight
+// is bfloat16, for its range, which a product with a scale needs.  A wave of one row block holds it in two such
+// numbers, the second what the first leaves, 2^-16 of each term: outputs are then off by their own rounding (1.6e-3
+// of them against 64 bits, one token over 1,000 keys; 2.5e-3 with one number).  That takes 24 vector instructions and the
+// products with V once more; us with two and one: 8.8 and 8.4 (that case), 116.5 and 115.3 (the pooled requests), 14.7 and
+// 13.9 (13 trees of 37-3,001 keys, D = 64), 83.5 and 77 (4 x 200,000 keys, D = 64).  Waves of more row blocks, bound by
+// their instructions, round it once (half a step: 2^-8 of each term; 2.2e-3 of the output where its rounding is
+// 1.7e-3): two numbers take 230 us instead of 164 (16 x 16,384-32,768 keys, 72 rows) and 145 instead of 111 (16 x 24,576, D = 64).
+// The 4-bit matrix instructions would take K without widening, but keep
 // too few bits of their sums: 6.6e-5 of the sum of magnitudes of 128 products, measured.
 //
 // Softmax in the log2 domain, against a reference that is the row's maximum as of the
@@ -34,8 +40,8 @@
 // rescaled, which a wave notices by the sums that it keeps anyway.  That happens outside the loop over the blocks:
 // inside, the compiler spills O, and a spill's reload waits for the DMAs before it.  Accumulators start
 // at -reference.  Where a reference is large (2^16 in the log2 domain: sums that start there round differently from those that
-// start at zero, by up to 2^-8 and, further up, by any factor), and for the block that sets it, scores are summed
-// from zero and the reference is subtracted from the sum: equal scores stay equal, and none exceeds its own maximum.
+// start at zero, by up to 2^-8 and, further up, by any factor), and in joined requests for the block that sets it, scores are
+// summed from zero and the reference is subtracted from the sum: equal scores stay equal, and none exceeds its own maximum.
 #include <algorithm>
 
 #include "fp4.h"
@@ -47,8 +53,8 @@ namespace sdv {
 namespace {
 
 constexpr int kMaxTiles4 = 64;   // blocks per chunk: one lane holds one block's page
-// Waves of a workgroup that takes a request.  Sixteen, on rings of one block: 9.8 us where eight take 8.9 (1,000
-// keys, one token, D = 128), 14.2 and 12.5 (4 x 1,500 keys, 72 rows).
+// Waves of a workgroup that takes a request.  Sixteen, on rings of one block (weights in one number): 9.8 us where
+// eight take 8.9 (1,000 keys, one token, D = 128), 14.2 and 12.5 (4 x 1,500 keys, 72 rows).
 constexpr int kJoinWaves = 8;
 constexpr int kManyChunks = 16;  // chunks of a request that one thread joins
 constexpr float kNoKey4 = -3.402823466e38f;  // reference of a row that has seen no key: no score lies below it
@@ -105,6 +111,28 @@ typedef __attribute__((__vector_size__(2 * sizeof(int)))) int i32x2;
 // points at: lane i of them gets column i, the codes in the order of the lanes.
 __device__ __forceinline__ i32x2 lds_read_tr4(const unsigned char* p) {
   return __builtin_amdgcn_ds_read_tr4_b64_v2i32((__attribute__((address_space(3))) i32x2*)p);
+}
+
+// bfloat16 numbers that a weight is held in for its products.
+template <int RB>
+constexpr int kParts = RB == 1 ? 2 : 1;
+
+// Four weights as two bfloat16 numbers each, from entry i on: rounded, and what that leaves of them, rounded.
+__device__ __forceinline__ void put_weights(bf16x8 (&pf)[2], int i, const float (&y)[4]) {
+  uint32_t first = 0x0000bf80u, second = 0xbf800000u;  // -1 and 0, 0 and -1, held in registers
+  asm("" : "+s"(first), "+s"(second));
+#pragma unroll
+  for (int r = 0; r < 4; r += 2) {
+    const bf16x2 hi = __builtin_convertvector((f32x2{y[r], y[r + 1]}), bf16x2);
+    const f32x2 rest = {__builtin_amdgcn_fdot2_f32_bf16(hi, __builtin_bit_cast(bf16x2, first), y[r], false),
+                        __builtin_amdgcn_fdot2_f32_bf16(hi, __builtin_bit_cast(bf16x2, second), y[r + 1], false)};
+    const bf16x2 lo = __builtin_convertvector(rest, bf16x2);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      pf[0][i + r + k] = hi[k];
+      pf[1][i + r + k] = lo[k];
+    }
+  }
 }
 
 template <int RB, int D>
@@ -215,7 +243,7 @@ __device__ __forceinline__ bool set_reference(Wave4<RB, D>& w, const unsigned ch
 
 // O += P V: V's columns come out of LDS transposed.
 template <int RB, int D>
-__device__ __forceinline__ void add_products4(Wave4<RB, D>& w, const unsigned char* vp, const bf16x8 (&pf)[RB][2]) {
+__device__ __forceinline__ void add_products4(Wave4<RB, D>& w, const unsigned char* vp, const bf16x8 (&pf)[RB][2][kParts<RB>]) {
   const int lane = lane_here(), lr = lane & 15, lg = lane >> 4;
   const unsigned char* vl = vp + (16 * (lr / 4) + 4 * lg + lr % 4) * 8;
   i32x2 v[D / 16];
@@ -228,8 +256,10 @@ __device__ __forceinline__ void add_products4(Wave4<RB, D>& w, const unsigned ch
     const bf16x8 now = vf;
     if (n + 1 < D / 8) vf = widen8_fp4((uint32_t)v[(n + 1) % (D / 16)][(n + 1) / (D / 16)], 1.f);  // under this fragment's products
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) w.o[rb][db] = mfma16x16x32(now, pf[rb][hf], w.o[rb][db]);
-    interleave4<RB, 4>();
+    for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+      for (int i = 0; i < kParts<RB>; ++i) w.o[rb][db] = mfma16x16x32(now, pf[rb][hf][i], w.o[rb][db]);
+    interleave4<RB * kParts<RB>, 4>();
   }
 }
 
@@ -246,7 +276,7 @@ __device__ __forceinline__ bool fold_block4(Wave4<RB, D>& w, const unsigned char
     sum[rb] = 0.f;
   }
   const uint32_t ks = key_scales4<D>(kp);
-  bf16x8 pf[RB][2];
+  bf16x8 pf[RB][2][kParts<RB>];
 #pragma unroll
   for (int hf = 0; hf < 2; ++hf) {
     f32x4 sc[RB][2];
@@ -266,7 +296,8 @@ __device__ __forceinline__ bool fold_block4(Wave4<RB, D>& w, const unsigned char
       }
     }
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+    for (int t = 0; t < 2; ++t) {
+      [[maybe_unused]] float ys[4];
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const uint32_t pair = vs[t][r / 2];
@@ -281,12 +312,17 @@ __device__ __forceinline__ bool fold_block4(Wave4<RB, D>& w, const unsigned char
             const uint32_t see = (uint32_t)(keys_seen(w.sees[rb], off) >> (32 * hf + 16 * t + r)) & 1u;
             y = __uint_as_float(see ? __float_as_uint(y) : 0u);
           }
-          pf[rb][hf][t * 4 + r] = (__bf16)y;
+          if constexpr (kParts<RB> == 1) pf[rb][hf][0][t * 4 + r] = (__bf16)y;
+          else ys[r] = y;
         }
       }
+      if constexpr (kParts<RB> == 2) put_weights(pf[0][hf], t * 4, ys);
+    }
     // The rounded weights are all that is kept of the scores.
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) asm volatile("" : "+v"(pf[rb][hf]));
+    for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+      for (int i = 0; i < kParts<RB>; ++i) asm volatile("" : "+v"(pf[rb][hf][i]));
   }
   bool grow = false;
 #pragma unroll
@@ -341,11 +377,12 @@ __device__ __forceinline__ bool fold_block_one(Wave4<1, D>& w, const unsigned ch
 #pragma unroll
       for (int r = 0; r < 4; ++r) sc[t / 2][0][t % 2][r] -= m;
   }
-  bf16x8 pf[1][2];
+  bf16x8 pf[1][2][2];
   float sum = 0.f;
   const uint64_t win = MASKED ? keys_seen(w.sees[0], off) : 0;
 #pragma unroll
-  for (int t = 0; t < 4; ++t)
+  for (int t = 0; t < 4; ++t) {
+    float ys[4];
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const float scale = __uint_as_float(r & 1 ? vs[t][r / 2] & 0xffff0000u : vs[t][r / 2] << 16);
@@ -357,8 +394,10 @@ __device__ __forceinline__ bool fold_block_one(Wave4<1, D>& w, const unsigned ch
         const uint32_t see = (uint32_t)(win >> (16 * t + r)) & 1u;
         y = __uint_as_float(see ? __float_as_uint(y) : 0u);
       }
-      pf[0][t / 2][t % 2 * 4 + r] = (__bf16)y;
+      ys[r] = y;
     }
+    put_weights(pf[0][t / 2], t % 2 * 4, ys);
+  }
   bool grow = sum > kGrow;
   if (MASKED) grow |= !(w.m[0] > kNoKey4) && (win & 0x000f000f000f000full) != 0;  // a row's first keys, whatever their weights
   if (__builtin_expect(__ballot(grow) != 0 && !set, 0)) return false;
@@ -544,7 +583,7 @@ __device__ __forceinline__ void store_four(uint16_t* out, const AttnShape& s, in
 }
 
 // The requests of a launch, longest first: workgroups that have to share a CU are then short ones (13 requests
-// of 37-3,001 keys, 312 workgroups: 14.1 us, 14.9 in the order of the batch).
+// of 37-3,001 keys, 312 workgroups: 14.6 us, 17.1 in the order of the batch).
 struct ByLength {
   uint8_t req[kMaxReqPerLaunch];
 };
@@ -601,10 +640,11 @@ void kv4_attn_join_kernel(AttnShape s, AttnBatch bt, Kv4Pool pool, ByLength orde
 
 // 16-row blocks of a wave, at most; more rows are split over row groups, a wave each.  `blocks`: 64-key
 // blocks times heads.  Where the caches are few blocks per CU, what counts is how long a wave takes for its own; where they are
-// many, that keys are read and widened once.  8 heads, requests of one length, us with at most 1, 2 and 5 row blocks:
-//   D = 128, 72 rows: 4 x 1,500 keys (750 blocks) 15.8, 17.8, 29.6; 64 x 1,500 (12,300) 88, 75, 66; 16 x 24,576 281, 221, 182
-//            40 rows: 24 x 1,400 (4,200) 27.9, 31.7, 36.5;  128 rows: 8 x 9,000 (9,000) 70.5, 64.9, 69.5
-//   D = 64:  48 rows: 13 x 1,500 (2,500) 16.5, 17.5, 19.9;  128 rows: 8 x 9,000 55.0, 48.3, 49.2;  72 rows: 16 x 24,576 152, 141, 126
+// many, that keys are read and widened once.  8 heads, requests of one length, cut into chunks, us with at most 1, 2 and 5
+// row blocks:
+//   D = 128, 72 rows: 4 x 1,500 keys (750 blocks) 15.8, 17.1, 25.6; 64 x 1,500 (12,300) 91, 70, 66; 16 x 24,576 314, 218, 154
+//            40 rows: 24 x 1,400 (4,200) 27.1, 27.6, 35.0;  128 rows: 8 x 9,000 (9,000) 77.5, 62.3, 66.7
+//   D = 64:  48 rows: 13 x 1,500 (2,500) 16.8, 19.0, 18.6;  128 rows: 8 x 9,000 60.8, 52.7, 46.5;  72 rows: 16 x 24,576 165, 129, 111
 int max_blocks4(int64_t blocks) { return blocks <= 24 * cu_count() ? 1 : blocks <= 40 * cu_count() ? 2 : 5; }
 int blocks_of4(int rows, int groups) { return ((rows + 15) / 16 + groups - 1) / groups; }
 
@@ -616,16 +656,16 @@ int64_t places4(int D, int most) {
 
 // What a wave of one to five row blocks takes for a block of keys by itself, and what each of the waves on a SIMD takes at
 // least, in ns, at head dimension 128 and 64: 50 blocks a wave, one wave and two per SIMD.
-constexpr int kAlone[2][5] = {{1340, 1630, 2100, 2600, 3100}, {700, 1280, 1370, 1800, 2100}};
-constexpr int kShared[2][5] = {{1300, 1530, 1920, 2750, 3200}, {700, 1020, 1270, 1780, 2150}};
+constexpr int kAlone[2][5] = {{1350, 1630, 2100, 2600, 3100}, {910, 1280, 1370, 1800, 2100}};
+constexpr int kShared[2][5] = {{1390, 1530, 1920, 2750, 3200}, {800, 1020, 1270, 1780, 2150}};
 
 // Whether requests are shared among the waves of one workgroup each (for 16 rows of a KV head)
 // instead of cut into chunks, which take `chunked` ns: by `groups` of those workgroups, the blocks of the longest
 // request, eight at once, and of all.  One launch less, against rows that are read once for each 16 and the longest
 // request's time.  In us, joined / in chunks, requests of one length, 8 KV heads; D = 128: 1 x 1,000 keys
-// 9.2 / 10.2, 1 x 4,000 18.5 / 10.4, 4 x 4,000 of 72 rows 19.5 / 23.4, 8 x 4,000 of one token 18.4 / 16.3,
-// 32 x 1,000 10.4 / 14.8; D = 64: 13 x 1,500 of 48 rows 13.1 / 17.4, 24 x 1,400 of 40 rows 16.9 / 20.4, 16 x 24,576 of
-// 72 rows 148 / 115.  Not of many more workgroups than run at once: 64 x 1,000 keys of one token, D = 128, 20.8 / 18.8.
+// 8.8-9.3 / 10.4, 1 x 4,000 20.9 / 10.5, 4 x 4,000 of 72 rows 21.3 / 24.1, 8 x 4,000 of one token 21.5 / 15.2,
+// 32 x 1,000 11.5 / 14.4; D = 64: 13 x 1,500 of 48 rows 13.0 / 16.8, 24 x 1,400 of 40 rows 17.5 / 21.3, 16 x 24,576 of
+// 72 rows 175 / 111.  Not of many more workgroups than run at once: 64 x 1,000 keys of one token, D = 128, 21.1 / 19.9.
 bool joins(int64_t groups, int64_t longest, int64_t total, int D, int64_t chunked) {
   if (longest > kJoinWaves * kMaxTiles4 || groups > (D == 128 ? cu_count() : cu_count() * 5 / 2)) return false;
   const int64_t all = total * kShared[D == 64][0] / (4 * cu_count());
@@ -634,8 +674,8 @@ bool joins(int64_t groups, int64_t longest, int64_t total, int D, int64_t chunke
 }
 
 // Joins many partials: the chunks of each (request, position, head) are dealt to the slices of a workgroup,
-// whose sums join in slice order.  A thread holds four columns.  One request of 30,000 keys in 60 chunks,
-// one token, D = 128: 21 us the whole call.
+// whose sums join in slice order.  A thread holds four columns.  One request of 30,000 keys, one token, 8 KV heads,
+// D = 128: 5.5 us of 17.8 with 32 query heads, in 118 chunks, and 8.3 of 20.3 with 8, in 235.
 template <int D>
 __global__ __launch_bounds__(256)
 void kv4_merge_many_kernel(AttnShape s, AttnBatch bt, AttnPartials parts, uint16_t* __restrict__ out) {
