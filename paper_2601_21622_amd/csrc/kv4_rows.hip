@@ -7,7 +7,8 @@
 // in each of the D / 16 column groups, and the two orders meet in LDS.
 //
 // Bound by memory where there are many keys: appending 8 prompts of 1 to 6,001 bf16 rows (8 heads, D = 128, 124 MB) takes
-// 26 us, 4.8 TB/s, and reading 8 sessions of 1 to 9,001 keys 39.5 us, 4.7 TB/s; a large copy's rate is 4.7-4.9.  With a dword
+// 26 us, 4.8 TB/s, and reading 8 sessions of 1 to 9,001 keys 39.5 us, 4.7 TB/s; a large copy's rate is 4.7-4.9.  In float32
+// they take 47.7 us, 4.7 TB/s, and 88.5 us, 3.8 TB/s.  With a dword
 // a thread and a wave per four keys, and no LDS, they took 40 and 71.  Steps of a few keys are bound by latency: 5 keys
 // of 64 requests, 32 heads, 5.5 us (table, rows and stores, one behind the other).
 #include <type_traits>
