@@ -31,7 +31,8 @@ _SCALES = (torch.bfloat16, torch.int16, torch.uint16)
 
 class KV4Cache(ctypes.Structure):
     """sd_kv4_cache_t: a 4-bit paged cache.  Build it with KV4Cache.of(...),
-    which checks the pools against each other and keeps them referenced as long as it lives."""
+    which checks the pools against each other and keeps them referenced as long as it
+    lives: a captured graph's calls need it alive for as long as the graph is replayed."""
     _fields_ = [
         ("k", ctypes.c_void_p),
         ("v", ctypes.c_void_p),

@@ -28,7 +28,8 @@ _TYPES = {SD_DTYPE_F32: torch.float32, SD_DTYPE_BF16: torch.bfloat16}
 
 class KV8Cache(ctypes.Structure):
     """sd_kv8_cache_t: an 8-bit paged cache.  Build it with KV8Cache.of(...),
-    which checks the pools against each other and keeps them referenced as long as it lives."""
+    which checks the pools against each other and keeps them referenced as long as it
+    lives: a captured graph's calls need it alive for as long as the graph is replayed."""
     _fields_ = [
         ("k", ctypes.c_void_p),
         ("v", ctypes.c_void_p),
